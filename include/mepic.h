@@ -408,6 +408,126 @@ int mepic_attn_decode_batched_workspace_size(const mepic_attn_params* params, co
 int mepic_attn_decode_batched(const mepic_attn_params* params, const int32_t* plan_device,
                               const mepic_decode_plan_info* info, void* hip_stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * Verification of drafted tokens over the same pages. A step appends a tree of drafted tokens to each request, runs the
+ * model on all of them at once and keeps the K/V of one path from the root. Per step: mepic_tables_extend (slots and, if wanted,
+ * pages for the drafted tokens), per layer mepic_kv_commit and mepic_attn_tree, and after the choice of the path mepic_kv_keep
+ * per layer. All lengths stay on the device, nothing waits for the host, and every call can be captured into a graph.
+ * ---------------------------------------------------------------------------------------------- */
+#define MEPIC_TREE_MAX_NODES 256
+
+/*
+ * Attention of a tree of drafted tokens over a paged cache (§3.3.3: the same fused rotation over un-rotated pages). The query
+ * tokens cu_q_lens[b] .. cu_q_lens[b+1]-1 of request b are the nodes 0 .. T-1 of its tree; their K/V are already committed
+ * and occupy the last T of the request's kv_lens[b] slots in order: node j sits in slot C + j, C = kv_lens[b] - T. A node sees
+ *   - every context slot n < C whose bit in block_valid_mask is set (when given); its position is block_positions[b][n / P] + s or n,
+ *     as for mepic_attn_decode, and no causal test is made: the context lies before the tree;
+ *   - the nodes on its path from the root, itself among them (their bits count, too). The K of node j is rotated at the position of its
+ *     query token, q_positions[cu_q_lens[b] + j], whatever its slot: siblings usually have equal positions.
+ *
+ *   parents: device int32 [n_q_tokens], the parent of each node as its number in the request's tree, always smaller than the
+ *   node's own; anything else (usually -1) makes the node a root. NULL: each request's nodes form a chain, node j - 1 is the parent of j.
+ *
+ * params as for mepic_attn_prefill (cu_q_lens and max_q_len as there; MEPIC_FLAG_FORCE_GENERAL runs plain fp32 arithmetic).
+ * Rows behind cu_q_lens[B] are left as they were. A row that sees no slot is all zeros. A request of more than max_q_len nodes, or
+ * of fewer slots than nodes, gives unspecified rows, never a fault. What a row does not see may hold anything, NaN and Inf included.
+ * 16-bit pages: keys are rotated in fp32 and enter matrix products as fp16 (11 significant bits), bf16 probabilities meet bf16 V as stored;
+ * e4m3 pages: everything in fp16. A row that comes out Inf or NaN is computed again in plain fp32 arithmetic.
+ * Errors: as mepic_attn_prefill, and MEPIC_ERR_UNSUPPORTED for max_q_len > MEPIC_TREE_MAX_NODES.
+ */
+int mepic_attn_tree(const mepic_attn_params* params, const int32_t* parents, void* hip_stream);
+
+/* Bytes of workspace mepic_attn_tree needs; reads what mepic_attn_workspace_size reads. */
+int mepic_attn_tree_workspace_size(const mepic_attn_params* params, size_t* bytes_out);
+
+/*
+ * Block tables, slot maps and positions of the tokens a step appends, from device-resident lengths (§3.2.3's block allocation, carried
+ * on where the host cannot know the lengths): request b gets new_lens[b] tokens in its slots kv_lens[b], kv_lens[b] + 1, ...; blocks it
+ * has no page for take the next pages of a list of free pages, requests in index order, blocks in ascending order.
+ *
+ * Tokens are packed, [cu_tokens[b], cu_tokens[b+1]) being request b's; cu_tokens, run_request and run_first_slot are what mepic_kv_commit
+ * takes as runs, cu_tokens is the cu_q_lens of mepic_attn_tree and mepic_attn_prefill.
+ *
+ * A request that cannot grow gets nothing: its status is not 0, run_request and run_first_slot are -1 (mepic_kv_commit and mepic_kv_keep
+ * leave it out), kv_lens_out and n_blocks_out repeat its old values, its tokens have slot, position and request -1; the
+ * others keep their places. A request needs pages in vain if the demand up to and with it exceeds the list (then so do all
+ * later ones that need any).
+ *
+ * n_blocks, n_blocks_out, free_pages, free_head, free_head_out: all or none. NULL: the tables already hold the pages (the
+ * pool's extra_tail_tokens, a plan ahead), and only the width of the table is checked.
+ * In place: *_out may be the very array it updates (kv_lens_out = kv_lens and so on). Other arrays must not overlap.
+ * Errors: MEPIC_ERR_INVALID (null pointers, negative sizes, some of the page-list arrays without the others, P not 1..32, misaligned
+ * workspace), MEPIC_ERR_CAPACITY (workspace), MEPIC_ERR_LAUNCH.
+ */
+enum { MEPIC_EXTEND_OK = 0, MEPIC_EXTEND_NO_BLOCKS = 1 /* table too narrow */, MEPIC_EXTEND_NO_PAGES = 2 /* list used up */,
+       MEPIC_EXTEND_BAD_LENGTH = 3 /* a negative length; counts as no tokens */ };
+
+typedef struct {
+  const int32_t* kv_lens;          /* device [B] slots in use                                                */
+  const int32_t* new_lens;         /* device [B] tokens to append                                            */
+  int32_t* block_tables;           /* device [B][max_blocks]; entries of newly assigned blocks are written   */
+  const int32_t* n_blocks;         /* device [B] blocks that have a page, or NULL                            */
+  const int32_t* free_pages;       /* device [n_free] page ids, or NULL                                      */
+  const int32_t* free_head;        /* device [1] entries of free_pages already used, or NULL                 */
+  const int32_t* first_positions;  /* device [B] position of the first new token, or NULL: kv_lens[b]        */
+  const int32_t* token_offsets;    /* device [max_tokens] added to it per token (a node's depth), or NULL:
+                                      the token's index among the request's new ones                         */
+  int32_t* kv_lens_out;            /* device [B]                                                             */
+  int32_t* n_blocks_out;           /* device [B], or NULL                                                    */
+  int32_t* free_head_out;          /* device [1], or NULL                                                    */
+  int32_t* cu_tokens;              /* device [B+1]                                                           */
+  int32_t* run_request;            /* device [B]                                                             */
+  int32_t* run_first_slot;         /* device [B]                                                             */
+  int32_t* status;                 /* device [B] MEPIC_EXTEND_*                                              */
+  int64_t* token_slots;            /* device [max_tokens] page * P + slot in the page, or NULL (-1 for a page
+                                      id outside [0, num_pages))                                             */
+  int32_t* token_positions;        /* device [max_tokens], or NULL                                           */
+  int32_t* token_requests;         /* device [max_tokens], or NULL                                           */
+  int32_t* block_positions;        /* device [B][max_blocks], or NULL: blocks whose slot 0 is new get the
+                                      position that continues from first_positions                           */
+  uint32_t* block_valid_mask;      /* device [B][max_blocks], or NULL: bits of new slots are set, the other
+                                      bits of blocks whose slot 0 is new are cleared                         */
+  int32_t B, max_blocks, P, num_pages;
+  int32_t n_free;                  /* entries of free_pages                                                  */
+  int32_t max_tokens;              /* room of the token arrays; tokens behind it are left out of them and of
+                                      block_positions / block_valid_mask, entries behind the last token keep
+                                      what they held                                                         */
+  void* workspace;                 /* device scratch, 256-byte aligned                                       */
+  size_t workspace_bytes;
+} mepic_extend_params;
+
+int mepic_tables_extend_workspace_size(const mepic_extend_params* params, size_t* bytes_out);
+int mepic_tables_extend(const mepic_extend_params* params, void* hip_stream);
+
+/*
+ * Keep one path of the tree: the K/V of the accepted nodes move to the slots right behind the context (§3.3.2's commit of what is
+ * already in pages), in every KV head. Of request b, whose node 0 sits in slot first_slots[b] and which has cu_tree[b+1] - cu_tree[b] nodes,
+ * kept[cu_kept[b]] .. kept[cu_kept[b+1]-1] are the accepted nodes in ascending order (a path from a root always is): the r-th goes
+ * to slot first_slots[b] + r. kv_lens_out[b], if given, becomes first_slots[b] + the number kept. fp32 and bf16 pages: a copy.
+ * e4m3 pages: a copy within a page and between pages of equal scale; otherwise mepic_kv_commit's quantisation of
+ * fp32(code) * source scale by the destination's scale.
+ * Left out, their destination keeping what it held: entries that are not larger than the one before, below their rank, or not in
+ * the tree; entries whose source or destination block or page id is out of range. Requests with first_slots[b] < 0 are left out, kv_lens_out
+ * too. Two requests that share the pages moved in race, as for mepic_kv_commit.
+ * Errors: as mepic_kv_commit.
+ */
+typedef struct {
+  void* k_pages;                   /* device, K page layout, kv_dtype                                        */
+  void* v_pages;                   /* device, V page layout, kv_dtype                                        */
+  const float* k_scales;           /* device [num_pages] fp32 > 0; required iff kv_dtype == F8E4M3           */
+  const float* v_scales;
+  const int32_t* block_tables;     /* device [B][max_blocks]                                                 */
+  const int32_t* first_slots;      /* device [B] slot of node 0, or negative: nothing to do                  */
+  const int32_t* cu_tree;          /* device [B+1] prefix sums of nodes per request                          */
+  const int32_t* kept;             /* device [n_kept] node numbers                                           */
+  const int32_t* cu_kept;          /* device [B+1] prefix sums of kept nodes per request, at most n_kept     */
+  int32_t* kv_lens_out;            /* device [B], or NULL                                                    */
+  int32_t B, n_kept, Hkv, D, P, max_blocks, num_pages;
+  int32_t kv_dtype;                /* F32 | BF16 | F8E4M3                                                    */
+} mepic_keep_params;
+
+int mepic_kv_keep(const mepic_keep_params* params, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -21,6 +21,8 @@ BLOCK_PRIVATE, BLOCK_SHARED_HIT, BLOCK_SHARED_NEW = 0, 1, 2
 F32, BF16, F8E4M3 = 0, 1, 2
 FLAG_ROPE_INTERLEAVED, FLAG_FORCE_GENERAL, FLAG_KV_READ_ONCE = 1, 2, 4
 NOALLOC_SCRATCH_BYTES = 48 << 20
+TREE_MAX_NODES = 256
+EXTEND_OK, EXTEND_NO_BLOCKS, EXTEND_NO_PAGES, EXTEND_BAD_LENGTH = 0, 1, 2, 3
 
 EXPORTS = ["mepic_strerror", "mepic_version", "mepic_pool_create", "mepic_pool_destroy", "mepic_align_request",
            "mepic_release_request", "mepic_pool_get_stats", "mepic_pool_lookup_chunk", "mepic_attn_workspace_size",
@@ -28,7 +30,8 @@ EXPORTS = ["mepic_strerror", "mepic_version", "mepic_pool_create", "mepic_pool_d
            "mepic_decode_plan_capacity", "mepic_decode_plan_build", "mepic_attn_decode_batched_workspace_size",
            "mepic_attn_decode_batched", "mepic_attn_decode_noalloc", "mepic_selftest_dot_rotation",
            "mepic_decode_plan_build_ahead", "mepic_probe_mfma_bf16", "mepic_device_counter_khz",
-           "mepic_probe_tile_stream"]
+           "mepic_probe_tile_stream", "mepic_attn_tree", "mepic_attn_tree_workspace_size", "mepic_tables_extend",
+           "mepic_tables_extend_workspace_size", "mepic_kv_keep"]
 
 
 class MepicError(RuntimeError):
@@ -86,6 +89,21 @@ class DecodePlanInfo(ctypes.Structure):
         return {n: int(getattr(self, n)) for n, _ in self._fields_}
 
 
+class ExtendParams(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("kv_lens", "new_lens", "block_tables", "n_blocks", "free_pages", "free_head",
+                                                "first_positions", "token_offsets", "kv_lens_out", "n_blocks_out", "free_head_out",
+                                                "cu_tokens", "run_request", "run_first_slot", "status", "token_slots",
+                                                "token_positions", "token_requests", "block_positions", "block_valid_mask")]
+                + [(n, ctypes.c_int32) for n in ("B", "max_blocks", "P", "num_pages", "n_free", "max_tokens")]
+                + [("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)])
+
+
+class KeepParams(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("k_pages", "v_pages", "k_scales", "v_scales", "block_tables", "first_slots",
+                                                "cu_tree", "kept", "cu_kept", "kv_lens_out")]
+                + [(n, ctypes.c_int32) for n in ("B", "n_kept", "Hkv", "D", "P", "max_blocks", "num_pages", "kv_dtype")])
+
+
 _lib = None
 
 
@@ -131,6 +149,11 @@ def load() -> ctypes.CDLL:
                                                              ctypes.POINTER(ctypes.c_size_t)]
     lib.mepic_attn_decode_batched.argtypes = [ctypes.POINTER(AttnParams), ctypes.c_void_p,
                                               ctypes.POINTER(DecodePlanInfo), ctypes.c_void_p]
+    lib.mepic_attn_tree.argtypes = [ctypes.POINTER(AttnParams), ctypes.c_void_p, ctypes.c_void_p]
+    lib.mepic_attn_tree_workspace_size.argtypes = [ctypes.POINTER(AttnParams), ctypes.POINTER(ctypes.c_size_t)]
+    lib.mepic_tables_extend.argtypes = [ctypes.POINTER(ExtendParams), ctypes.c_void_p]
+    lib.mepic_tables_extend_workspace_size.argtypes = [ctypes.POINTER(ExtendParams), ctypes.POINTER(ctypes.c_size_t)]
+    lib.mepic_kv_keep.argtypes = [ctypes.POINTER(KeepParams), ctypes.c_void_p]
     _lib = lib
     return lib
 
@@ -402,6 +425,135 @@ def kv_commit(params: CommitParams, stream=None) -> None:
     rc = load().mepic_kv_commit(ctypes.byref(params), _stream_handle(stream))
     if rc != OK:
         raise MepicError(rc, "mepic_kv_commit")
+
+
+# ------------------------------------------------------------------------------------------------
+# verification of drafted tokens
+# ------------------------------------------------------------------------------------------------
+def _want(what: str, t, dtype, shape, device) -> None:
+    """`t` is a tensor of that type, shape (None: any extent) and device, or ValueError."""
+    if t.dtype != dtype or t.dim() != len(shape) or any(w is not None and n != w for n, w in zip(t.shape, shape)) or t.device != device:
+        raise ValueError(f"{what}: {dtype} of shape {tuple(shape)} on {device} expected, got {t.dtype} of shape {tuple(t.shape)} on {t.device}")
+
+
+def attn_tree_workspace_size(params: AttnParams) -> int:
+    n = ctypes.c_size_t()
+    rc = load().mepic_attn_tree_workspace_size(ctypes.byref(params), ctypes.byref(n))
+    if rc != OK:
+        raise MepicError(rc, "mepic_attn_tree_workspace_size")
+    return int(n.value)
+
+
+def attn_tree(params: AttnParams, parents=None, stream=None) -> None:
+    """mepic_attn_tree on `stream` (default: torch's current stream). params: make_params with cu_q_lens and max_q_len; parents:
+    int32 tensor [n_q_tokens] on the GPU, None for chains."""
+    if parents is not None and (parents.numel() != params.n_q_tokens or parents.element_size() != 4):
+        raise ValueError(f"parents: int32 of shape ({params.n_q_tokens},) expected, got {parents.dtype} of shape {tuple(parents.shape)}")
+    rc = load().mepic_attn_tree(ctypes.byref(params), _p(parents), _stream_handle(stream))
+    if rc != OK:
+        raise MepicError(rc, "mepic_attn_tree")
+
+
+def make_extend_params(kv_lens, new_lens, block_tables, *, P: int, num_pages: int, kv_lens_out, cu_tokens, run_request, run_first_slot,
+                       status, n_blocks=None, n_blocks_out=None, free_pages=None, free_head=None, free_head_out=None, first_positions=None,
+                       token_offsets=None, token_slots=None, token_positions=None, token_requests=None, block_positions=None,
+                       block_valid_mask=None, max_tokens: Optional[int] = None, workspace=None) -> ExtendParams:
+    """Fill a mepic_extend_params from torch tensors laid out as include/mepic.h states (int32, token_slots int64, the mask uint32 or
+    int32). max_tokens: by default the length of the token arrays."""
+    import torch
+    (B,), dev, i32 = kv_lens.shape, kv_lens.device, torch.int32
+    _want("kv_lens", kv_lens, i32, (B,), dev)
+    _want("block_tables", block_tables, i32, (B, None), dev)
+    for what, t in (("new_lens", new_lens), ("kv_lens_out", kv_lens_out), ("run_request", run_request), ("run_first_slot", run_first_slot),
+                    ("status", status), ("n_blocks", n_blocks), ("n_blocks_out", n_blocks_out), ("first_positions", first_positions)):
+        if t is not None:
+            _want(what, t, i32, (B,), dev)
+    _want("cu_tokens", cu_tokens, i32, (B + 1,), dev)
+    for what, t in (("free_head", free_head), ("free_head_out", free_head_out)):
+        if t is not None:
+            _want(what, t, i32, (1,), dev)
+    if free_pages is not None:
+        _want("free_pages", free_pages, i32, (None,), dev)
+    tokens = [("token_offsets", token_offsets, i32), ("token_slots", token_slots, torch.int64), ("token_positions", token_positions, i32),
+              ("token_requests", token_requests, i32)]
+    lengths = [t.shape[0] for _, t, _ in tokens if t is not None]
+    n = max_tokens if max_tokens is not None else min(lengths, default=0)
+    for what, t, dt in tokens:
+        if t is not None:
+            _want(what, t, dt, (None,), dev)
+            if t.shape[0] < n:
+                raise ValueError(f"{what}: room for {t.shape[0]} tokens, {n} expected")
+    if (block_positions is not None or block_valid_mask is not None) and not lengths and max_tokens is None:
+        raise ValueError("block_positions and block_valid_mask are written per token: give max_tokens")
+    if block_positions is not None:
+        _want("block_positions", block_positions, i32, block_tables.shape, dev)
+    if block_valid_mask is not None:
+        _want("block_valid_mask", block_valid_mask, i32 if block_valid_mask.dtype == i32 else torch.uint32, block_tables.shape, dev)
+    p = ExtendParams()
+    given = dict(kv_lens=kv_lens, new_lens=new_lens, block_tables=block_tables, n_blocks=n_blocks, free_pages=free_pages, free_head=free_head,
+                 first_positions=first_positions, token_offsets=token_offsets, kv_lens_out=kv_lens_out, n_blocks_out=n_blocks_out,
+                 free_head_out=free_head_out, cu_tokens=cu_tokens, run_request=run_request, run_first_slot=run_first_slot, status=status,
+                 token_slots=token_slots, token_positions=token_positions, token_requests=token_requests, block_positions=block_positions,
+                 block_valid_mask=block_valid_mask)
+    for name, t in given.items():
+        setattr(p, name, _p(t))
+    p.B, p.max_blocks, p.P, p.num_pages, p.max_tokens = B, block_tables.shape[1], P, num_pages, n
+    p.n_free = 0 if free_pages is None else free_pages.shape[0]
+    if workspace is not None:
+        p.workspace, p.workspace_bytes = _p(workspace), workspace.numel() * workspace.element_size()
+    # the struct holds raw device pointers: keep the tensors alive for as long as it is
+    p._tensors = (given, workspace)
+    return p
+
+
+def tables_extend_workspace_size(params: ExtendParams) -> int:
+    n = ctypes.c_size_t()
+    rc = load().mepic_tables_extend_workspace_size(ctypes.byref(params), ctypes.byref(n))
+    if rc != OK:
+        raise MepicError(rc, "mepic_tables_extend_workspace_size")
+    return int(n.value)
+
+
+def tables_extend(params: ExtendParams, stream=None) -> None:
+    """mepic_tables_extend on `stream` (default: torch's current stream)."""
+    rc = load().mepic_tables_extend(ctypes.byref(params), _stream_handle(stream))
+    if rc != OK:
+        raise MepicError(rc, "mepic_tables_extend")
+
+
+def make_keep_params(k_pages, v_pages, block_tables, first_slots, cu_tree, kept, cu_kept, *, k_scales=None, v_scales=None,
+                     kv_lens_out=None) -> KeepParams:
+    """Fill a mepic_keep_params from torch tensors laid out as include/mepic.h states."""
+    import torch
+    B, dev, i32 = block_tables.shape[0], k_pages.device, torch.int32
+    num_pages, Hkv, D, P = v_pages.shape
+    X = 16 // k_pages.element_size()
+    _want("k_pages", k_pages, v_pages.dtype, (num_pages, Hkv, D // X, P, X), dev)
+    _want("v_pages", v_pages, k_pages.dtype, (num_pages, Hkv, D, P), dev)
+    _want("block_tables", block_tables, i32, (B, None), dev)
+    for what, t, n in (("first_slots", first_slots, B), ("cu_tree", cu_tree, B + 1), ("kept", kept, None), ("cu_kept", cu_kept, B + 1),
+                       ("kv_lens_out", kv_lens_out, B)):
+        if t is not None:
+            _want(what, t, i32, (n,), dev)
+    for what, t in (("k_scales", k_scales), ("v_scales", v_scales)):
+        if t is not None:
+            _want(what, t, torch.float32, (num_pages,), dev)
+    p = KeepParams()
+    p.k_pages, p.v_pages, p.k_scales, p.v_scales = _p(k_pages), _p(v_pages), _p(k_scales), _p(v_scales)
+    p.block_tables, p.first_slots, p.cu_tree, p.kept, p.cu_kept = _p(block_tables), _p(first_slots), _p(cu_tree), _p(kept), _p(cu_kept)
+    p.kv_lens_out = _p(kv_lens_out)
+    p.B, p.n_kept, p.Hkv, p.D, p.P, p.max_blocks, p.num_pages = B, kept.numel(), Hkv, D, P, block_tables.shape[1], num_pages
+    p.kv_dtype = _dt(k_pages)
+    # the struct holds raw device pointers: keep the tensors alive for as long as it is
+    p._tensors = (k_pages, v_pages, k_scales, v_scales, block_tables, first_slots, cu_tree, kept, cu_kept, kv_lens_out)
+    return p
+
+
+def kv_keep(params: KeepParams, stream=None) -> None:
+    """mepic_kv_keep on `stream` (default: torch's current stream)."""
+    rc = load().mepic_kv_keep(ctypes.byref(params), _stream_handle(stream))
+    if rc != OK:
+        raise MepicError(rc, "mepic_kv_keep")
 
 
 # ------------------------------------------------------------------------------------------------

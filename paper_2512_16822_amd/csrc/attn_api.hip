@@ -1,10 +1,12 @@
 // C-ABI entry points of the attention half of the library: argument checks, the split-K plan, the
 // rotary frequency table, and dispatch to the kernels. No device memory is allocated here.
+#include <climits>
 #include <cmath>
 #include <cstring>
 #include <mutex>
 
 #include "attn_common.h"
+#include "tree_common.h"
 
 // Scratch of mepic_attn_decode_noalloc: the split-K partials and their metadata live here instead of in a
 // caller-supplied workspace. Every GPU the library runs on holds its own copy of the array, at its own address,
@@ -298,10 +300,64 @@ int run_batched(const mepic_attn_params* p, const int32_t* plan, const mepic_dec
   return e == hipSuccess ? MEPIC_OK : MEPIC_ERR_LAUNCH;
 }
 
+// Attention of a tree: prefill's checks and argument block.
+int run_tree(const mepic_attn_params* p, const int32_t* parents, void* hip_stream, size_t* bytes_only) {
+  const int rc = check_shapes(p, true);
+  if (rc != MEPIC_OK) return rc;
+  const int max_q = p->max_q_len > 0 && p->max_q_len < p->n_q_tokens ? p->max_q_len : p->n_q_tokens;
+  if (max_q > MEPIC_TREE_MAX_NODES || (long)p->n_q_tokens * p->Hq > INT_MAX) return MEPIC_ERR_UNSUPPORTED;
+  const size_t need = 0;
+  if (bytes_only) {
+    *bytes_only = need;
+    return MEPIC_OK;
+  }
+  if (p->n_q_tokens == 0) return MEPIC_OK;
+  if (!p->q || !p->out || !p->k_pages || !p->v_pages || !p->block_tables || !p->kv_lens || !p->q_positions || !p->cu_q_lens || p->B == 0)
+    return MEPIC_ERR_INVALID;
+  if (p->kv_dtype == MEPIC_F8E4M3 && (!p->k_scales || !p->v_scales)) return MEPIC_ERR_INVALID;
+  if (!(p->rope_theta > 0.f)) return MEPIC_ERR_INVALID;
+  if ((p->timing_start == nullptr) != (p->timing_stop == nullptr)) return MEPIC_ERR_INVALID;
+  if (need && (!p->workspace || p->workspace_bytes < need)) return MEPIC_ERR_CAPACITY;
+  if (reinterpret_cast<uintptr_t>(p->workspace) & 255u) return MEPIC_ERR_INVALID;
+
+  TreeArgs t{};
+  AttnArgs& a = t.a;
+  a.timing_start = p->timing_start; a.timing_stop = p->timing_stop;
+  a.q = p->q; a.out = p->out; a.k_pages = p->k_pages; a.v_pages = p->v_pages;
+  a.k_scales = p->k_scales; a.v_scales = p->v_scales;
+  a.block_tables = p->block_tables; a.kv_lens = p->kv_lens; a.q_positions = p->q_positions; a.cu_q_lens = p->cu_q_lens;
+  a.block_positions = p->block_positions; a.block_valid_mask = p->block_valid_mask;
+  a.B = p->B; a.n_q = p->n_q_tokens; a.Hq = p->Hq; a.Hkv = p->Hkv; a.D = p->D; a.P = p->P;
+  a.max_blocks = p->max_blocks; a.num_pages = p->num_pages; a.G = p->Hq / p->Hkv;
+  a.q_dtype = p->q_dtype; a.kv_dtype = p->kv_dtype;
+  a.interleaved = (p->flags & MEPIC_FLAG_ROPE_INTERLEAVED) ? 1 : 0;
+  a.kv_read_once = (p->flags & MEPIC_FLAG_KV_READ_ONCE) ? 1 : 0;
+  const double sm = p->sm_scale > 0.f ? (double)p->sm_scale : 1.0 / std::sqrt((double)p->D);
+  a.qk_scale_log2 = (float)(sm * 1.4426950408889634);
+  fill_frequencies(p, &a);
+  t.parents = parents;
+  t.max_q = max_q;
+  hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
+  g_last_kernel = "tree_general";
+  mark(a.timing_start, s);
+  const hipError_t e = launch_tree_general(t, s);
+  mark(a.timing_stop, s);
+  return e == hipSuccess ? MEPIC_OK : MEPIC_ERR_LAUNCH;
+}
+
 }  // namespace
 }  // namespace mepic
 
 extern "C" {
+
+int mepic_attn_tree_workspace_size(const mepic_attn_params* params, size_t* bytes_out) {
+  if (!bytes_out) return MEPIC_ERR_INVALID;
+  return mepic::run_tree(params, nullptr, nullptr, bytes_out);
+}
+
+int mepic_attn_tree(const mepic_attn_params* params, const int32_t* parents, void* hip_stream) {
+  return mepic::run_tree(params, parents, hip_stream, nullptr);
+}
 
 int mepic_attn_decode_batched_workspace_size(const mepic_attn_params* params, const mepic_decode_plan_info* info,
                                              size_t* bytes_out) {
