@@ -306,7 +306,15 @@ int run_tree(const mepic_attn_params* p, const int32_t* parents, void* hip_strea
   if (rc != MEPIC_OK) return rc;
   const int max_q = p->max_q_len > 0 && p->max_q_len < p->n_q_tokens ? p->max_q_len : p->n_q_tokens;
   if (max_q > MEPIC_TREE_MAX_NODES || (long)p->n_q_tokens * p->Hq > INT_MAX) return MEPIC_ERR_UNSUPPORTED;
-  const size_t need = 0;
+  TreeArgs t{};
+  AttnArgs& a = t.a;
+  a.B = p->B; a.n_q = p->n_q_tokens; a.Hq = p->Hq; a.Hkv = p->Hkv; a.D = p->D; a.P = p->P;
+  a.max_blocks = p->max_blocks; a.num_pages = p->num_pages; a.G = p->Hq / p->Hkv;
+  t.max_q = max_q;
+  int max_kv = p->max_kv_len > 0 ? p->max_kv_len : p->max_blocks * p->P;
+  if (max_kv > p->max_blocks * p->P) max_kv = p->max_blocks * p->P;
+  const TreePlan pl = p->kv_dtype == MEPIC_F32 || (p->flags & MEPIC_FLAG_FORCE_GENERAL) ? TreePlan{} : tree_mfma_plan(t, max_kv);
+  const size_t need = pl.bytes;
   if (bytes_only) {
     *bytes_only = need;
     return MEPIC_OK;
@@ -320,15 +328,11 @@ int run_tree(const mepic_attn_params* p, const int32_t* parents, void* hip_strea
   if (need && (!p->workspace || p->workspace_bytes < need)) return MEPIC_ERR_CAPACITY;
   if (reinterpret_cast<uintptr_t>(p->workspace) & 255u) return MEPIC_ERR_INVALID;
 
-  TreeArgs t{};
-  AttnArgs& a = t.a;
   a.timing_start = p->timing_start; a.timing_stop = p->timing_stop;
   a.q = p->q; a.out = p->out; a.k_pages = p->k_pages; a.v_pages = p->v_pages;
   a.k_scales = p->k_scales; a.v_scales = p->v_scales;
   a.block_tables = p->block_tables; a.kv_lens = p->kv_lens; a.q_positions = p->q_positions; a.cu_q_lens = p->cu_q_lens;
   a.block_positions = p->block_positions; a.block_valid_mask = p->block_valid_mask;
-  a.B = p->B; a.n_q = p->n_q_tokens; a.Hq = p->Hq; a.Hkv = p->Hkv; a.D = p->D; a.P = p->P;
-  a.max_blocks = p->max_blocks; a.num_pages = p->num_pages; a.G = p->Hq / p->Hkv;
   a.q_dtype = p->q_dtype; a.kv_dtype = p->kv_dtype;
   a.interleaved = (p->flags & MEPIC_FLAG_ROPE_INTERLEAVED) ? 1 : 0;
   a.kv_read_once = (p->flags & MEPIC_FLAG_KV_READ_ONCE) ? 1 : 0;
@@ -336,12 +340,17 @@ int run_tree(const mepic_attn_params* p, const int32_t* parents, void* hip_strea
   a.qk_scale_log2 = (float)(sm * 1.4426950408889634);
   fill_frequencies(p, &a);
   t.parents = parents;
-  t.max_q = max_q;
   hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
-  g_last_kernel = "tree_general";
+  hipError_t e;
   mark(a.timing_start, s);
-  const hipError_t e = launch_tree_general(t, s);
-  mark(a.timing_stop, s);
+  if (pl.rows) {
+    g_last_kernel = p->kv_dtype == MEPIC_F8E4M3 ? "tree_mfma_fp8" : "tree_mfma_bf16";
+    e = launch_tree_mfma(t, pl, p->workspace, s);
+  } else {
+    g_last_kernel = "tree_general";
+    e = launch_tree_general(t, s);
+    mark(a.timing_stop, s);
+  }
   return e == hipSuccess ? MEPIC_OK : MEPIC_ERR_LAUNCH;
 }
 

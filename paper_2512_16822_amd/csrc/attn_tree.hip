@@ -1,22 +1,12 @@
-// Attention of a tree of drafted tokens, general form: every case the call allows, in plain fp32 arithmetic. One workgroup per output
-// row; it is what the matrix-core kernels fall back to for rows that came out Inf or NaN.
+// Attention of a tree of drafted tokens: the general kernel (every case the call allows, in plain fp32 arithmetic, one workgroup per
+// output row), and of the matrix-core kernels the plan, the merge of rows that several workgroups share, and the dispatch.
+#include "merge_partials.h"
 #include "tree_common.h"
 
 namespace mepic {
 namespace {
 
 constexpr int kRowThreads = 256;
-
-// The request that owns query token t, or -1 for a row behind the last one (the prefix sums ascend; empty requests own nothing).
-__device__ __forceinline__ int request_of(const int32_t* cu, int B, int t) {
-  if (t >= cu[B] || t < cu[0]) return -1;
-  int lo = 0, hi = B;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (cu[mid] <= t) lo = mid; else hi = mid;
-  }
-  return lo;
-}
 
 template <int KV>
 __global__ __launch_bounds__(kRowThreads) void tree_general_kernel(const TreeArgs ta) {
@@ -29,7 +19,132 @@ __global__ __launch_bounds__(kRowThreads) void tree_general_kernel(const TreeArg
   tree_row<KV, kRowThreads>(ta, lds, r, b, t - r.q0, hq);
 }
 
+// Rows whose item was cut: the partials of workgroups first .. last, the first one's in its second slot, the others' in their first. Groups of
+// D / 4 threads, a thread four dims; each group has a row of its own, or (kOneRow) all take every kGroups-th partial of one row.
+template <int KV, int D, bool kOneRow>
+__global__ __launch_bounds__(kRowThreads) void tree_merge_kernel(const TreeMfmaArgs m, int rows) {
+  constexpr int kCols = D / 4, kGroups = kRowThreads / kCols;
+  __shared__ float4 num_s[kGroups][kCols];
+  __shared__ float2 ml_s[kGroups];
+  __shared__ int bad[kGroups];
+  __shared__ TreeRowLds<kRowThreads> lds;
+  const AttnArgs& a = m.t.a;
+  const int grp = threadIdx.x / kCols, col = threadIdx.x % kCols;
+  const int row = kOneRow ? blockIdx.x : blockIdx.x * kGroups + grp;
+  const int t = row / a.Hq, hq = row - t * a.Hq, hk = hq / a.G;
+  const bool here = row < a.n_q * a.Hq && t < a.cu_q_lens[a.B];
+  int4 w = make_int4(0, 0, 0, 0);
+  if (here) w = m.row_wgs[(size_t)t * a.G + hq - hk * a.G];
+  // (a request that breaks max_q_len has rows nobody wrote: whatever is there forms no address outside the workspace)
+  const int first = min(max(w.x, 0), m.groups - 1), last = min(max(w.y, first), m.groups - 1), in = min(max(w.z, 0), rows - 1);
+  const bool cut = here && last > first;
+  if (kOneRow && !cut) return;
+  float top = -INFINITY, den = 0.f;
+  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto add = [&](const float2& e, const float4& y) {
+    if (e.x == -INFINITY && e.y == 0.f) return;  // no slot took part
+    const float now = fmaxf(top, e.x);
+    const float f = now == top ? 1.f : __builtin_amdgcn_exp2f(top - now), u = now == e.x ? 1.f : __builtin_amdgcn_exp2f(e.x - now);
+    top = now;
+    den = den * f + u * e.y;
+    x.x = x.x * f + u * y.x; x.y = x.y * f + u * y.y; x.z = x.z * f + u * y.z; x.w = x.w * f + u * y.w;
+  };
+  auto part = [&](int s) { return (((size_t)s * a.Hkv + hk) * 2 + (s == first ? 1 : 0)) * rows + in; };
+  if (cut) {
+    constexpr int kStep = kOneRow ? kGroups : 1;
+    for (int s = first + (kOneRow ? grp : 0); s <= last; s += 4 * kStep) {
+      float2 e[4];
+      float4 y[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const size_t p = part(min(s + i * kStep, last));
+        e[i] = *reinterpret_cast<const float2*>(m.part_ml + 2 * p);
+        y[i] = *reinterpret_cast<const float4*>(m.part_o + p * D + 4 * col);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (s + i * kStep <= last) add(e[i], y[i]);
+    }
+  }
+  if constexpr (kOneRow) {
+    num_s[grp][col] = x;
+    if (col == 0) ml_s[grp] = make_float2(top, den);
+    __syncthreads();
+    top = -INFINITY; den = 0.f;
+    x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < kGroups; ++i) add(ml_s[i], num_s[i][col]);
+  }
+  if (col == 0) bad[grp] = 0;
+  __syncthreads();
+  if (cut && (!kOneRow || grp == 0)) {
+    const float inv = den != 0.f ? 1.f / den : 0.f;
+    uint2 v;
+    v.x = pack2_bf16(x.x * inv, x.y * inv);
+    v.y = pack2_bf16(x.z * inv, x.w * inv);
+    __builtin_memcpy(static_cast<uint16_t*>(a.out) + (size_t)row * D + 4 * col, &v, 8);
+    const float odd = (x.x + x.y + x.z + x.w) * 0.f + den * 0.f;
+    if (!(odd == 0.f)) bad[grp] = 1;
+  }
+  __syncthreads();
+  for (int i = 0; i < (kOneRow ? 1 : kGroups); ++i) {
+    if (!bad[i]) continue;
+    const int r = kOneRow ? (int)blockIdx.x : (int)blockIdx.x * kGroups + i, tok = r / a.Hq, b = request_of(a.cu_q_lens, a.B, tok);
+    if (b < 0) continue;
+    const TreeRequest rq = tree_request(a, b);
+    if (tok - rq.q0 < m.t.max_q) tree_row<KV, kRowThreads>(m.t, lds, rq, b, tok - rq.q0, r - tok * a.Hq);
+  }
+}
+
+template <int KV, int D>
+void launch_merge(const TreeMfmaArgs& m, int rows, hipStream_t s) {
+  const int n = m.t.a.n_q * m.t.a.Hq;
+  if (n <= 1024) {
+    tree_merge_kernel<KV, D, true><<<n, kRowThreads, 0, s>>>(m, rows);
+  } else {
+    constexpr int per = kRowThreads / (D / 4);
+    tree_merge_kernel<KV, D, false><<<(n + per - 1) / per, kRowThreads, 0, s>>>(m, rows);
+  }
+}
+
 }  // namespace
+
+TreePlan tree_mfma_plan(const TreeArgs& t, int max_kv) {
+  const AttnArgs& a = t.a;
+  TreePlan p{};
+  if (a.max_blocks == 0 || a.num_pages == 0 || a.B == 0) return p;  // (no page to read)
+  const long row_bound = (long)t.max_q * a.G;
+  p.rows = row_bound <= 32 ? 32 : row_bound <= 64 ? 64 : row_bound <= 128 ? 128 : 256;
+  const int cus = device_compute_units();
+  p.groups = cus / a.Hkv > 1 ? cus / a.Hkv : 1;
+  const long tiles = (max_kv + kTreeTile - 1) / kTreeTile;
+  if (((long)a.n_q * a.G / p.rows + a.B + 1) * (tiles + 1) > (1L << 30)) return TreePlan{};  // (the work is counted in 32 bits)
+  p.whole = tiles <= 4;
+  p.min_tiles = 2;
+  if (!p.whole)
+    p.bytes = (size_t)p.groups * a.Hkv * 2 * p.rows * (a.D + 2) * sizeof(float) + (size_t)a.n_q * a.G * sizeof(int4);
+  return p;
+}
+
+hipError_t launch_tree_mfma(const TreeArgs& t, const TreePlan& pl, void* workspace, hipStream_t s) {
+  const AttnArgs& a = t.a;
+  TreeMfmaArgs m{};
+  m.t = t;
+  m.groups = pl.groups; m.min_tiles = pl.min_tiles; m.whole = pl.whole;
+  const size_t parts = (size_t)pl.groups * a.Hkv * 2 * pl.rows;
+  m.row_wgs = static_cast<int4*>(workspace);
+  m.part_o = reinterpret_cast<float*>(m.row_wgs + (size_t)a.n_q * a.G);
+  m.part_ml = m.part_o + parts * a.D;
+  const bool fp8 = a.kv_dtype == MEPIC_F8E4M3;
+  hipError_t e = fp8 ? launch_tree_tiles_fp8(pl.rows, m, s) : launch_tree_tiles_bf16(pl.rows, m, s);
+  if (a.timing_stop) (void)hipEventRecord(reinterpret_cast<hipEvent_t>(a.timing_stop), s);
+  if (e != hipSuccess || pl.whole) return e;
+  if (fp8 && a.D == 128) launch_merge<MEPIC_F8E4M3, 128>(m, pl.rows, s);
+  else if (fp8) launch_merge<MEPIC_F8E4M3, 64>(m, pl.rows, s);
+  else if (a.D == 128) launch_merge<MEPIC_BF16, 128>(m, pl.rows, s);
+  else launch_merge<MEPIC_BF16, 64>(m, pl.rows, s);
+  return hipGetLastError();
+}
 
 hipError_t launch_tree_general(const TreeArgs& t, hipStream_t s) {
   const dim3 grid((unsigned)t.a.n_q * t.a.Hq);

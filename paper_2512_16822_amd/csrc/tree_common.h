@@ -24,8 +24,8 @@ struct TreeRequest {
 
 __device__ __forceinline__ TreeRequest tree_request(const AttnArgs& a, int b) {
   TreeRequest r;
-  r.q0 = a.cu_q_lens[b];
-  r.T = max(a.cu_q_lens[b + 1] - r.q0, 0);
+  r.q0 = min(max(a.cu_q_lens[b], 0), a.n_q);  // (nothing on the device is taken on trust where it forms an address)
+  r.T = min(max(a.cu_q_lens[b + 1] - r.q0, 0), a.n_q - r.q0);
   r.kv_len = max(min(a.kv_lens[b], a.max_blocks * a.P), 0);
   r.ctx = r.kv_len - r.T;
   return r;
@@ -174,6 +174,39 @@ __device__ __forceinline__ void tree_row(const TreeArgs& ta, TreeRowLds<kThreads
   }
 }
 
+// The request that owns query token t, or -1 for a row behind the last one (the prefix sums ascend; empty requests own nothing).
+__device__ __forceinline__ int request_of(const int32_t* cu, int B, int t) {
+  if (t >= cu[B] || t < cu[0]) return -1;
+  int lo = 0, hi = B;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (cu[mid] <= t) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+
+// How a call of the matrix-core kernels is cut (tree_mfma_plan).
+struct TreePlan {
+  int rows;        // rows of a workgroup's tile: 32, 64, 128, 256
+  int groups;      // workgroups per KV head
+  int min_tiles;   // least run of a workgroup, in tiles of kTreeTile slots
+  bool whole;      // a workgroup takes whole items (row tiles of a request): nothing to merge
+  size_t bytes;    // workspace
+};
+constexpr int kTreeTile = 128;
+
+struct TreeMfmaArgs {
+  TreeArgs t;
+  int32_t groups, min_tiles, whole;
+  float* part_o;     // [groups * Hkv][2][rows][D]
+  float* part_ml;    // [groups * Hkv][2][rows][2]
+  int4* row_wgs;     // [n_q * G] first and last workgroup (of a KV head) that a row's item is cut for, row of the tile, request
+};
+
+TreePlan tree_mfma_plan(const TreeArgs& t, int max_kv);  // reads shapes and max_q; rows = 0: the general kernel's
+hipError_t launch_tree_mfma(const TreeArgs& t, const TreePlan& pl, void* workspace, hipStream_t s);  // bf16 or e4m3 pages; with its merge and timing_stop
+hipError_t launch_tree_tiles_bf16(int rows, const TreeMfmaArgs& m, hipStream_t s);
+hipError_t launch_tree_tiles_fp8(int rows, const TreeMfmaArgs& m, hipStream_t s);
 hipError_t launch_tree_general(const TreeArgs& t, hipStream_t s);  // any form, plain fp32 arithmetic
 
 }  // namespace mepic

@@ -1,0 +1,609 @@
+// Attention of a tree of drafted tokens on the matrix cores, bf16 and e4m3 pages: the kernel, a template that the attn_tree_*.hip
+// files instantiate.
+//
+// A verification step brings R = nodes x (Hq / Hkv) query rows per KV head to the same context: 8 to 512 where decode has 1 to 16. So
+// a key is rotated once per tile of rows and shared through LDS, and HBM bounds the call up to some 128 rows.
+//   * Work. An item is a tile of kRows rows of one request; its keys come in tiles of 128 slots. The (item, tile) pairs of a KV head form
+//     one sequence that the head's workgroups (one per compute unit, 8 waves) cut into equal runs; a row cut in two
+//     or more goes through partials and tree_merge_kernel, any other is written directly.
+//   * Staging. A thread has one slot and D / 4 dims of it: whole rotary pairs. cos and sin of its slot's position stay in registers and are
+//     turned on by 128 positions from tile to tile (the turn is the same for a wave: scalar registers), found anew every 16 tiles and where
+//     positions jump. K goes to LDS as fp16 in operand order, V as matrix operands too (e4m3 widened to fp16, which holds the codes
+//     exactly); the loads of the next tile are in flight during the products of this one.
+//   * Products. S^T[32 slots x 16 rows] = K Q^T with v_mfma_f32_16x16x32_f16 and O^T[dims x rows] += V^T P^T: a lane owns one row, so
+//     sums, maxima and rescaling are its own. Slots are laid out so that the scores a lane gets are the eight consecutive slots its
+//     operand of P^T needs. kGroups groups of waves take 16 kTiles rows each; waves of a group share the tile's slots and are merged in
+//     LDS at the end of a run.
+//   * Precision. Query rows are scaled by a power of two to at most 1 and keys times 16 (e4m3 codes as they are), both in fp16: 11
+//     significant bits where bf16 has 8; a key beyond 2896 gives an infinite score, which marks the row. P is bf16 next to bf16 V, fp16
+//     next to e4m3 V, where the exponent of the page's V scale joins the score and its mantissa P. Sums and O are fp32. The reference maximum
+//     of a row lags by up to 8 (log2 units).
+//   * A marked row, or one that came out Inf or NaN, is computed again by tree_row.
+#pragma once
+#include "lanes.h"
+#include "tree_common.h"
+
+namespace mepic {
+
+constexpr int kTreeThreads = 512;
+constexpr int kReseed = 16;  // tiles after which cos and sin are found anew
+
+struct TreeLdsTail {  // behind the two tile buffers
+  float freq[2][kMaxHalfD];
+  uint32_t path[MEPIC_TREE_MAX_NODES][kTreeWords];
+  int16_t parent[MEPIC_TREE_MAX_NODES];
+  uint32_t valid[2][4];
+  float scale[2][2][8];  // K and V scale of the tile's blocks (e4m3)
+  float ml[8][32][2];
+  int bad[256];
+  int scan[16];
+  int found[2];
+  TreeRowLds<kTreeThreads> row;
+};
+
+template <int D> constexpr size_t tree_lds_bytes() { return 2 * (size_t)kTreeTile * D * 2 * 2 + sizeof(TreeLdsTail); }
+
+__device__ __forceinline__ uint32_t pack2_f16(float lo, float hi) {
+  const f32x2 v = {lo, hi};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2));
+}
+
+// The low n bits, n from anything below 0 to anything above 32.
+__device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u; }
+
+// Bits of slots n0 .. n0 + 31 that a row sees: all of the context's, of the nodes those on its path.
+__device__ __forceinline__ uint32_t path_bits(const uint32_t* path, int n0, int ctx) {
+  const int off = n0 - ctx;  // bit i is node off + i
+  if (off <= -32) return ~0u;
+  if (off < 0) return low_bits(-off) | (path[0] << -off);
+  const int w = off >> 5, s = off & 31;
+  const uint32_t lo = w < kTreeWords ? path[w] >> s : 0u;
+  return s && w + 1 < kTreeWords ? lo | (path[w + 1] << (32 - s)) : lo;
+}
+
+template <bool kFp8, int D, int kGroups, int kTiles, bool kInter>
+__global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeMfmaArgs m) {
+  constexpr int kRows = kGroups * kTiles * 16, kSlotGroups = 8 / kGroups, kSubs = 4 / kSlotGroups;
+  constexpr int kSteps = D / 32, kDims = D / 16;          // products per score, 16-dim tiles of O
+  constexpr int E = kFp8 ? 1 : 2, X = 16 / E, DX = D / X;  // bytes per element, elements per granule
+  constexpr int NL = D / 8;                               // rotary pairs per thread: NL low and NL high dims of one slot
+  constexpr int kKeyBytes = kTreeTile * D * 2, kTileBytes = 2 * kKeyBytes;
+  constexpr int kVGranules = 16 * D * E / 16 / 64;        // 16-byte pieces of V per lane and tile
+  constexpr float kKeyFactor = kFp8 ? 1.f : 16.f;
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+  TreeLdsTail& tail = *reinterpret_cast<TreeLdsTail*>(lds + 2 * kTileBytes);
+  const TreeArgs& ta = m.t;
+  const AttnArgs& a = ta.a;
+  const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), n16 = lane & 15, g = lane >> 4;
+  const int hk = blockIdx.x % a.Hkv, wg = blockIdx.x / a.Hkv, G = a.G, P = a.P, logP = P == 16 ? 4 : 5;
+  const int rg = wave % kGroups, sg = wave / kGroups;
+
+  if (tid < D / 2) {
+    tail.freq[0][tid] = a.freq_hi[tid];
+    tail.freq[1][tid] = a.freq_lo[tid];
+  }
+
+  // ---- this workgroup's run: [begin, end) of the (item, tile) pairs of all requests ----
+  auto cost_of = [&](int b, int& tiles, int& items) {
+    const TreeRequest r = tree_request(a, b);
+    tiles = max((r.kv_len + kTreeTile - 1) / kTreeTile, 1);
+    items = (min(r.T, ta.max_q) * G + kRows - 1) / kRows;
+    return m.whole ? items : items * tiles;
+  };
+  // inclusive prefix sums of the costs of 512 requests; returns their total
+  auto scan_costs = [&](int b0, int& incl, int& cost) {
+    int tiles, items;
+    cost = b0 + tid < a.B ? cost_of(b0 + tid, tiles, items) : 0;
+    incl = cost;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int y = __shfl_up(incl, o);
+      if (lane >= o) incl += y;
+    }
+    if (lane == 63) tail.scan[wave] = incl;
+    __syncthreads();
+    int before = 0, total = 0;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) {
+      const int x = tail.scan[w];
+      if (w < wave) before += x;
+      total += x;
+    }
+    incl += before;
+    __syncthreads();
+    return total;
+  };
+  int incl, cost, total = scan_costs(0, incl, cost);
+  for (int b0 = kTreeThreads; b0 < a.B; b0 += kTreeThreads) {
+    int i2, c2;
+    total += scan_costs(b0, i2, c2);
+  }
+  const int per = max((total + m.groups - 1) / m.groups, m.whole ? 1 : m.min_tiles);
+  int at = wg * per;
+  const int end = min(total, at + per);
+  if (at >= end) return;
+  int b = 0, before = 0;  // the request of `at`, and the cost of those in front of it
+  {
+    int base = 0, sum = a.B > kTreeThreads ? scan_costs(0, incl, cost) : total;
+    for (int b0 = 0;; ) {
+      if (cost > 0 && base + incl - cost <= at && at < base + incl) {
+        tail.found[0] = b0 + tid;
+        tail.found[1] = base + incl - cost;
+      }
+      if (at < base + sum) break;
+      base += sum;
+      b0 += kTreeThreads;
+      sum = scan_costs(b0, incl, cost);
+    }
+    __syncthreads();
+    b = uni(tail.found[0]);
+    before = uni(tail.found[1]);
+  }
+
+  // ---- what a thread stages: slot `sl` of the tile, pairs of dims of quarter pc (pc is the wave's) ----
+  const int pc = wave >> 1, place = tid & 127;
+  const int sl = (place & ~31) | ((place & 12) << 1) | ((place & 16) >> 2) | (place & 3);
+  float turn_c[NL], turn_s[NL];  // the turn from tile to tile (the same for the wave)
+  auto freq_index = [&](int e) { return kInter ? (e < NL / 2 ? pc * (NL / 2) + e : D / 4 + pc * (NL / 2) + e - NL / 2) : pc * NL + e; };
+#pragma unroll
+  for (int e = 0; e < NL; ++e) {
+    const int i = freq_index(e);
+    const float f = turns_frac((float)kTreeTile, a.freq_hi[i], a.freq_lo[i]);
+    turn_c[e] = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(__builtin_amdgcn_cosf(f))));
+    turn_s[e] = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(__builtin_amdgcn_sinf(f))));
+  }
+  const int v_page = wave >> (logP - 4), v_first = (wave & ((P >> 4) - 1)) * (64 * kVGranules);
+  const size_t page_bytes = (size_t)a.Hkv * D * P * E, head_bytes = (size_t)hk * D * P * E;
+  const unsigned char* kp = static_cast<const unsigned char*>(a.k_pages) + head_bytes;
+  const unsigned char* vp = static_cast<const unsigned char*>(a.v_pages) + head_bytes;
+
+  while (at < end) {
+    const TreeRequest r = tree_request(a, b);
+    int tiles, items;
+    const int mine = cost_of(b, tiles, items);
+    if (at >= before + mine) {  // on to the next request
+      before += mine;
+      if (++b >= a.B) return;
+      continue;
+    }
+    const int rt = m.whole ? at - before : (at - before) / tiles;
+    const int t0 = m.whole ? 0 : at - before - rt * tiles;
+    const int t1 = m.whole ? tiles : min(tiles, t0 + end - at);
+    const int n_rows = min(r.T, ta.max_q) * G - rt * kRows;  // rows from the item's first to the request's last
+    const size_t bt_row = (size_t)b * a.max_blocks;
+
+    // rows that other workgroups share: which ones (head 0 says so for all)
+    if (!m.whole && t0 == 0 && hk == 0) {
+      const int last = (before + rt * tiles + tiles - 1) / per;
+      for (int i = tid; i < min(n_rows, kRows); i += kTreeThreads) {
+        m.row_wgs[(size_t)r.q0 * G + rt * kRows + i] = make_int4(wg, last, i, b);
+      }
+    }
+    // paths, where the run has nodes among its slots
+    const bool nodes_here = t1 * kTreeTile > r.ctx;
+    if (nodes_here) {
+      const int T = min(r.T, MEPIC_TREE_MAX_NODES);
+      if (tid < T) tail.parent[tid] = (int16_t)tree_parent(ta.parents, r.q0, tid);
+      __syncthreads();
+      if (tid < T) {
+#pragma unroll
+        for (int w = 0; w < kTreeWords; ++w) tail.path[tid][w] = 0;
+        int word = tid >> 5;
+        uint32_t bits = 0;
+        for (int j = tid; j >= 0; j = tail.parent[j]) {  // (numbers fall along a path)
+          if ((j >> 5) != word) {
+            tail.path[tid][word] = bits;
+            word = j >> 5;
+            bits = 0;
+          }
+          bits |= 1u << (j & 31);
+        }
+        tail.path[tid][word] = bits;
+      }
+    }
+
+    // ---- loads of a tile: page ids, positions and masks a tile ahead of the data ----
+    struct Ids { int k_page, v_page, s_page, pos; uint32_t k_mask, v_mask, s_mask, word; float ks, vs; };
+    auto load_ids = [&](int t) {
+      Ids x;
+      const int n = t * kTreeTile + sl, blk = min(n >> logP, a.max_blocks - 1);
+      const int vblk = min(((t * kTreeTile) >> logP) + v_page, a.max_blocks - 1);
+      x.k_page = a.block_tables[bt_row + blk];
+      x.v_page = a.block_tables[bt_row + vblk];
+      x.pos = n;
+      if (n >= r.ctx) x.pos = a.q_positions[min(max(r.q0 + n - r.ctx, 0), a.n_q - 1)];
+      else if (a.block_positions) x.pos = a.block_positions[bt_row + blk] + (n & (P - 1));
+      x.k_mask = x.v_mask = x.s_mask = x.word = ~0u;
+      const int sblk = min(((t * kTreeTile) >> logP) + (tid & 7), a.max_blocks - 1);  // (threads 0 .. 7: the blocks of the tile)
+      if (kFp8) x.s_page = a.block_tables[bt_row + sblk];
+      if (a.block_valid_mask) {
+        x.k_mask = a.block_valid_mask[bt_row + blk];
+        x.v_mask = a.block_valid_mask[bt_row + vblk];
+        if (kFp8) x.s_mask = a.block_valid_mask[bt_row + sblk];
+        if (tid < 4) {  // thread i: the 32 slots of group i
+          const int w0 = min((t * kTreeTile + 32 * tid) >> logP, a.max_blocks - 1);
+          x.word = a.block_valid_mask[bt_row + w0];
+          if (P == 16) x.word = (x.word & 0xffffu) | (a.block_valid_mask[bt_row + min(w0 + 1, a.max_blocks - 1)] << 16);
+        }
+      }
+      x.ks = x.vs = 0.f;
+      return x;
+    };
+    struct Data { uint4 k[kFp8 ? (NL >= 16 ? 2 : 1) : 2 * NL / 8]; uint4 v[kVGranules]; };
+    auto load_data = [&](Data& d, Ids& x, int t) {
+      const size_t pk = (size_t)max(min(x.k_page, a.num_pages - 1), 0) * page_bytes, pv = (size_t)max(min(x.v_page, a.num_pages - 1), 0) * page_bytes;
+      const int s = (t * kTreeTile + sl) & (P - 1);
+      if constexpr (kFp8 && NL == 8) {  // eight low and eight high codes
+        const int c = pc >> 1, o = (pc & 1) * 8;
+        const uint2 lo = *reinterpret_cast<const uint2*>(kp + pk + ((size_t)(c * P + s)) * 16 + o);
+        const uint2 hi = *reinterpret_cast<const uint2*>(kp + pk + ((size_t)((c + DX / 2) * P + s)) * 16 + o);
+        d.k[0] = make_uint4(lo.x, lo.y, hi.x, hi.y);
+      } else {
+        constexpr int kPer = NL / X;  // granules of low dims
+#pragma unroll
+        for (int c = 0; c < kPer; ++c) {
+          d.k[c] = *reinterpret_cast<const uint4*>(kp + pk + ((size_t)((pc * kPer + c) * P + s)) * 16);
+          d.k[kPer + c] = *reinterpret_cast<const uint4*>(kp + pk + ((size_t)((DX / 2 + pc * kPer + c) * P + s)) * 16);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kVGranules; ++i) d.v[i] = *reinterpret_cast<const uint4*>(vp + pv + (size_t)(v_first + 64 * i + lane) * 16);
+      if constexpr (kFp8) {
+        if (tid < 8) {
+          const int page = max(min(x.s_page, a.num_pages - 1), 0);
+          x.ks = a.k_scales[page];
+          x.vs = a.v_scales[page];
+        }
+      }
+    };
+
+    // ---- queries of the wave's rows ----
+    Frag q[kTiles][kSteps];
+    float row_scale[kTiles];
+    int row_node[kTiles];
+#pragma unroll
+    for (int nr = 0; nr < kTiles; ++nr) {
+      const int row = rt * kRows + (rg * kTiles + nr) * 16 + n16, node = row / G, head = row - node * G;
+      const bool there = node < min(r.T, ta.max_q);
+      row_node[nr] = there ? min(node, MEPIC_TREE_MAX_NODES - 1) : 0;
+      float x[kSteps][8];
+      const uint16_t* src = static_cast<const uint16_t*>(a.q) + ((size_t)(r.q0 + row_node[nr]) * a.Hq + (size_t)hk * G + head) * D;
+      const float pos = there ? (float)a.q_positions[r.q0 + row_node[nr]] : 0.f;
+#pragma unroll
+      for (int kk = 0; kk < kSteps; ++kk) {
+        uint4 u = make_uint4(0, 0, 0, 0);
+        if (there) __builtin_memcpy(&u, src + 8 * (4 * kk + g), 16);
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          x[kk][2 * j] = __uint_as_float(w[j] << 16);
+          x[kk][2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+        }
+      }
+      auto turned = [&](float& lo, float& hi, int i) {
+        const float f = turns_frac(pos, tail.freq[0][i], tail.freq[1][i]);
+        const float c = __builtin_amdgcn_cosf(f), s = __builtin_amdgcn_sinf(f);
+        const float y = lo * c - hi * s;
+        hi = hi * c + lo * s;
+        lo = y;
+      };
+      float most = 0.f;
+#pragma unroll
+      for (int kk = 0; kk < kSteps; ++kk)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if constexpr (kInter) {
+            if (j % 2 == 0) turned(x[kk][j], x[kk][j + 1], 4 * (4 * kk + g) + j / 2);
+          } else {
+            if (kk < kSteps / 2) turned(x[kk][j], x[kk + kSteps / 2][j], 8 * (4 * kk + g) + j);
+          }
+        }
+#pragma unroll
+      for (int kk = 0; kk < kSteps; ++kk)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(x[kk][j]));
+      most = max_over_kgroups(most);
+      const int e = most > 0.f ? max(__builtin_amdgcn_frexp_expf(most), -100) : 0;
+      row_scale[nr] = ldexpf(a.qk_scale_log2 / kKeyFactor, e);
+#pragma unroll
+      for (int kk = 0; kk < kSteps; ++kk)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) q[nr][kk].w[j] = pack2_f16(ldexpf(x[kk][2 * j], -e), ldexpf(x[kk][2 * j + 1], -e));
+    }
+
+    floatx4 o[kTiles][kDims];
+    float top[kTiles], ref[kTiles], sum[kTiles], least[kTiles];  // reference maximum, the same or 0, sum of weights, least score
+#pragma unroll
+    for (int nr = 0; nr < kTiles; ++nr) {
+      top[nr] = -INFINITY;
+      ref[nr] = sum[nr] = 0.f;
+      least[nr] = INFINITY;
+#pragma unroll
+      for (int dt = 0; dt < kDims; ++dt) o[nr][dt] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+    const bool busy = (rg * kTiles) * 16 < n_rows;  // does the wave have rows?
+
+    float cs[NL], sn[NL];
+    int pos_now = 0;
+    Data d;
+    Ids now = load_ids(t0);
+    load_data(d, now, t0);
+    Ids next = load_ids(min(t0 + 1, t1 - 1));
+
+    for (int t = t0; t < t1; ++t) {
+      unsigned char* buf = lds + (t & 1) * kTileBytes;
+      const int n = t * kTreeTile + sl, slots_left = r.kv_len - t * kTreeTile;
+      // -- stage tile t --
+      const bool live = n < r.kv_len && ((now.k_mask >> (n & (P - 1))) & 1u);
+      const int pos = n < r.kv_len ? now.pos : pos_now + kTreeTile;
+      const bool on = t != t0 && ((t - t0) & (kReseed - 1)) && __all(pos == pos_now + kTreeTile);
+      pos_now = pos;
+      if (on) {
+#pragma unroll
+        for (int e = 0; e < NL; ++e) {
+          const float c = cs[e] * turn_c[e] - sn[e] * turn_s[e];
+          sn[e] = sn[e] * turn_c[e] + cs[e] * turn_s[e];
+          cs[e] = c;
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < NL; ++e) {
+          const int i = freq_index(e);
+          const float f = turns_frac((float)pos, a.freq_hi[i], a.freq_lo[i]);
+          cs[e] = kKeyFactor * __builtin_amdgcn_cosf(f);
+          sn[e] = kKeyFactor * __builtin_amdgcn_sinf(f);
+        }
+      }
+      float x[2 * NL];  // low dims, then high ones
+      if constexpr (kFp8) {
+#pragma unroll
+        for (int c = 0; c < NL / 8; ++c) {
+          const uint32_t w[4] = {d.k[c].x, d.k[c].y, d.k[c].z, d.k[c].w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const f32x2 p = __builtin_amdgcn_cvt_pk_f32_fp8(w[j], false), q2 = __builtin_amdgcn_cvt_pk_f32_fp8(w[j], true);
+            x[16 * c + 4 * j] = p[0]; x[16 * c + 4 * j + 1] = p[1]; x[16 * c + 4 * j + 2] = q2[0]; x[16 * c + 4 * j + 3] = q2[1];
+          }
+        }
+      } else {
+#pragma unroll
+        for (int c = 0; c < 2 * NL / 8; ++c) {
+          const uint32_t w[4] = {d.k[c].x, d.k[c].y, d.k[c].z, d.k[c].w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            x[8 * c + 2 * j] = __uint_as_float(w[j] << 16);
+            x[8 * c + 2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+          }
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < NL; ++e) {
+        const int lo = kInter ? 2 * e : e, hi = kInter ? 2 * e + 1 : NL + e;
+        const float y = x[lo] * cs[e] - x[hi] * sn[e];
+        x[hi] = x[hi] * cs[e] + x[lo] * sn[e];
+        x[lo] = y;
+      }
+      Frag kf[2 * NL / 8];
+#pragma unroll
+      for (int c = 0; c < 2 * NL / 8; ++c)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) kf[c].w[j] = pack2_f16(x[8 * c + 2 * j], x[8 * c + 2 * j + 1]);
+      if (!__all(live)) {  // slots that take no part may hold anything
+#pragma unroll
+        for (int c = 0; c < 2 * NL / 8; ++c)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) kf[c].w[j] = live ? kf[c].w[j] : 0u;
+      }
+#pragma unroll
+      for (int c = 0; c < NL / 8; ++c) {
+        *reinterpret_cast<uint4*>(buf + ((pc * (NL / 8) + c) * kTreeTile + place) * 16) = kf[c].u;
+        *reinterpret_cast<uint4*>(buf + ((D / 16 + pc * (NL / 8) + c) * kTreeTile + place) * 16) = kf[NL / 8 + c].u;
+      }
+      // V: a granule is X consecutive slots of one dim, one or two operands of eight
+      const int v_slot = v_page << logP, v_left = slots_left - v_slot;  // slots of the page below kv_len
+      const uint32_t v_bits = now.v_mask & low_bits(v_left);
+      const bool v_whole = (v_bits | ~low_bits(P)) == ~0u;
+#pragma unroll
+      for (int i = 0; i < kVGranules; ++i) {
+        const int gi = v_first + 64 * i + lane, per_dim = P / X, dim = gi / per_dim, part = gi % per_dim;
+        Frag f[X / 8];
+        if constexpr (kFp8) {
+          const uint32_t w[4] = {d.v[i].x, d.v[i].y, d.v[i].z, d.v[i].w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const f32x2 p = __builtin_amdgcn_cvt_pk_f32_fp8(w[j], false), q2 = __builtin_amdgcn_cvt_pk_f32_fp8(w[j], true);
+            f[j / 2].w[2 * (j & 1)] = pack2_f16(p[0], p[1]);
+            f[j / 2].w[2 * (j & 1) + 1] = pack2_f16(q2[0], q2[1]);
+          }
+        } else {
+          f[0].u = d.v[i];
+        }
+#pragma unroll
+        for (int h = 0; h < X / 8; ++h) {
+          const int oct = part * (X / 8) + h;  // of the page
+          if (!v_whole) {
+            const uint32_t keep = v_bits >> (8 * oct);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              f[h].w[j] &= ((keep >> (2 * j)) & 1u ? 0x0000ffffu : 0u) | ((keep >> (2 * j + 1)) & 1u ? 0xffff0000u : 0u);
+          }
+          const int octet = (v_slot >> 3) + oct, twist = P == 16 ? (octet & 1) << 3 : (octet & 3) << 2;
+          *reinterpret_cast<uint4*>(buf + kKeyBytes + (octet * D + (dim ^ twist)) * 16) = f[h].u;
+        }
+      }
+      if (tid < 4) tail.valid[t & 1][tid] = now.word & low_bits(slots_left - 32 * tid);
+      if constexpr (kFp8) {
+        if (tid < 8) {
+          // (a block none of whose slots takes part may have any scale; a K scale of 0 would make NaN of the scores masked later)
+          const bool used = (now.s_mask & low_bits(min(slots_left - (tid << logP), P))) != 0;
+          tail.scale[t & 1][0][tid] = !used ? 1.f : now.ks == 0.f ? 1e-30f : now.ks;
+          tail.scale[t & 1][1][tid] = used ? now.vs : 0.f;
+        }
+      }
+      // -- the next tile's loads --
+      if (t + 1 < t1) {
+        now = next;
+        load_data(d, now, t + 1);
+        next = load_ids(min(t + 2, t1 - 1));
+      }
+      __syncthreads();
+
+      // -- products --
+      if (busy) {
+#pragma unroll 1
+        for (int sub = 0; sub < kSubs; ++sub) {
+          const int grp = sg * kSubs + sub, n0 = t * kTreeTile + 32 * grp;
+          floatx4 s[kTiles][2];
+#pragma unroll
+          for (int nr = 0; nr < kTiles; ++nr) s[nr][0] = s[nr][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int kk = 0; kk < kSteps; ++kk)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              Frag k;
+              k.u = *reinterpret_cast<const uint4*>(buf + ((4 * kk + g) * kTreeTile + 32 * grp + 16 * h + n16) * 16);
+#pragma unroll
+              for (int nr = 0; nr < kTiles; ++nr) s[nr][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k.hv, q[nr][kk].hv, s[nr][h], 0, 0, 0);
+            }
+          const uint32_t word = uni(tail.valid[t & 1][grp]);
+          const bool some = word != ~0u || n0 + 32 > r.ctx;
+          float ks = 1.f, ve = 0.f, vm = 1.f, vi = 1.f;  // K scale, V scale = 2^ve vm, vi = 2^-ve
+          if constexpr (kFp8) {
+            const int blk = P == 16 ? 2 * grp + (g >> 1) : grp;
+            ks = tail.scale[t & 1][0][blk];
+            const float vs = tail.scale[t & 1][1][blk];
+            const int e = min(max(__builtin_amdgcn_frexp_expf(vs), -100), 100);
+            ve = (float)e;
+            vm = ldexpf(vs, -e);
+            vi = ldexpf(1.f, -e);
+          }
+          Frag p[kTiles];
+#pragma unroll
+          for (int nr = 0; nr < kTiles; ++nr) {
+            float y[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = s[nr][j >> 2][j & 3];
+            if constexpr (!kFp8) {
+#pragma unroll
+              for (int j = 0; j < 8; ++j) least[nr] = fminf(least[nr], y[j]);
+            }
+            if (some) {
+              const uint32_t bits = (word & path_bits(tail.path[row_node[nr]], n0, r.ctx)) >> (8 * g);
+#pragma unroll
+              for (int j = 0; j < 8; ++j) y[j] = (bits >> j) & 1u ? y[j] : -INFINITY;
+            }
+            const float c = row_scale[nr] * ks;
+            float most = y[0];
+#pragma unroll
+            for (int j = 1; j < 8; ++j) most = fmaxf(most, y[j]);
+            most = most == -INFINITY ? most : __builtin_fmaf(most, c, ve);
+            if (__any(most > top[nr] + 8.f)) {
+              const float now_top = fmaxf(top[nr], max_over_kgroups(most));
+              const float f = now_top == top[nr] ? 1.f : __builtin_amdgcn_exp2f(top[nr] - now_top);
+              top[nr] = now_top;
+              ref[nr] = now_top == -INFINITY ? 0.f : now_top;
+              sum[nr] *= f;
+#pragma unroll
+              for (int dt = 0; dt < kDims; ++dt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[nr][dt][i] *= f;
+            }
+            const float shift = ve - ref[nr];
+            float part = 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              y[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(y[j], c, shift));
+              part += y[j];
+            }
+            if constexpr (kFp8) {
+              sum[nr] = __builtin_fmaf(part, vi, sum[nr]);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) p[nr].w[j] = pack2_f16(y[2 * j] * vm, y[2 * j + 1] * vm);
+            } else {
+              sum[nr] += part;
+#pragma unroll
+              for (int j = 0; j < 4; ++j) p[nr].w[j] = pack2_bf16(y[2 * j], y[2 * j + 1]);
+            }
+          }
+          const int twist = P == 16 ? (g & 1) << 3 : g << 2;
+#pragma unroll
+          for (int dt = 0; dt < kDims; ++dt) {
+            Frag v;
+            v.u = *reinterpret_cast<const uint4*>(buf + kKeyBytes + ((4 * grp + g) * D + ((16 * dt + n16) ^ twist)) * 16);
+#pragma unroll
+            for (int nr = 0; nr < kTiles; ++nr) {
+              if constexpr (kFp8) o[nr][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v.hv, p[nr].hv, o[nr][dt], 0, 0, 0);
+              else o[nr][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.v, p[nr].v, o[nr][dt], 0, 0, 0);
+            }
+          }
+        }
+      }
+    }
+
+    // ---- the waves of a group of rows merged, rows written ----
+    __syncthreads();  // (the last tile's operands are read)
+    const int rows_here = min(n_rows, kRows);
+    if (busy) {
+#pragma unroll
+      for (int nr = 0; nr < kTiles; ++nr) {
+        const float total_w = sum_over_kgroups(sum[nr]);
+        const float low = -max_over_kgroups(-least[nr]);
+        const int row = nr * 16 + n16;
+        if (g == 0) {
+          tail.ml[wave][row][0] = top[nr];
+          tail.ml[wave][row][1] = low == -INFINITY ? NAN : total_w;
+        }
+        float* dst = reinterpret_cast<float*>(lds) + (size_t)(wave * kTiles * 16 + row) * D;
+#pragma unroll
+        for (int dt = 0; dt < kDims; ++dt) *reinterpret_cast<floatx4*>(dst + 4 * ((4 * dt + g) ^ n16)) = o[nr][dt];
+      }
+    }
+    for (int i = tid; i < kRows; i += kTreeThreads) tail.bad[i] = 0;
+    __syncthreads();
+    const bool direct = t0 == 0 && t1 == tiles;
+    constexpr int kQuads = D / 4;
+    const size_t part = ((size_t)blockIdx.x * 2 + (t0 == 0 ? 1 : 0)) * kRows;
+    for (int u = tid; u < rows_here * kQuads; u += kTreeThreads) {
+      const int row = u / kQuads, quad = u % kQuads, in = row % (16 * kTiles), w0 = row / (16 * kTiles);
+      float mx = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < kSlotGroups; ++i) mx = fmaxf(mx, tail.ml[w0 + i * kGroups][in][0]);
+      float den = 0.f;
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int i = 0; i < kSlotGroups; ++i) {
+        const int w = w0 + i * kGroups;
+        const float mi = tail.ml[w][in][0], li = tail.ml[w][in][1];
+        if (mi == -INFINITY && li == 0.f) continue;  // no slot took part
+        const float f = mi == mx ? 1.f : __builtin_amdgcn_exp2f(mi - mx);
+        const float4 y = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(lds) + (size_t)(w * kTiles * 16 + in) * D + 4 * (quad ^ (in & 15)));
+        den += f * li;
+        x.x += f * y.x; x.y += f * y.y; x.z += f * y.z; x.w += f * y.w;
+      }
+      if (direct) {
+        const int all = rt * kRows + row, node = all / G, head = all - node * G;
+        const float inv = den != 0.f ? 1.f / den : 0.f;
+        uint2 w;
+        w.x = pack2_bf16(x.x * inv, x.y * inv);
+        w.y = pack2_bf16(x.z * inv, x.w * inv);
+        __builtin_memcpy(static_cast<uint16_t*>(a.out) + ((size_t)(r.q0 + node) * a.Hq + (size_t)hk * G + head) * D + 4 * quad, &w, 8);
+        const float odd = (x.x + x.y + x.z + x.w) * 0.f + den * 0.f;  // NaN if anything is Inf or NaN
+        if (!(odd == 0.f)) tail.bad[row] = 1;
+      } else {
+        *reinterpret_cast<float4*>(m.part_o + (part + row) * D + 4 * quad) = x;
+        if (quad == 0) *reinterpret_cast<float2*>(m.part_ml + (part + row) * 2) = make_float2(mx, den);
+      }
+    }
+    __syncthreads();
+    if (direct) {
+      for (int row = 0; row < rows_here; ++row) {
+        if (!tail.bad[row]) continue;
+        const int all = rt * kRows + row, node = all / G, head = all - node * G;
+        tree_row<kFp8 ? MEPIC_F8E4M3 : MEPIC_BF16, kTreeThreads>(ta, tail.row, r, b, node, hk * G + head);
+      }
+    }
+    at += m.whole ? 1 : t1 - t0;
+  }
+}
+
+}  // namespace mepic
