@@ -5,10 +5,10 @@
 namespace mepic {
 namespace {
 
-template <int D, int kGroups, int kTiles, bool kInter>
+template <int D, int kGroups, int kTiles, bool kPlain>
 hipError_t launch_one(const TreeMfmaArgs& m, hipStream_t s) {
   static std::atomic<uint64_t> asked{0};
-  const auto kernel = tree_tiles_kernel<false, D, kGroups, kTiles, kInter>;
+  const auto kernel = tree_tiles_kernel<false, D, kGroups, kTiles, kPlain>;
   constexpr size_t bytes = tree_lds_bytes<D>();
   const hipError_t e = allow_lds(reinterpret_cast<const void*>(kernel), bytes, asked);
   if (e != hipSuccess) return e;
@@ -16,20 +16,20 @@ hipError_t launch_one(const TreeMfmaArgs& m, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <int D, bool kInter>
+template <int D, bool kPlain>
 hipError_t launch_rows(int rows, const TreeMfmaArgs& m, hipStream_t s) {
-  if (rows == 32) return launch_one<D, 2, 1, kInter>(m, s);
-  if (rows == 64) return launch_one<D, 2, 2, kInter>(m, s);
-  if (rows == 128) return launch_one<D, 4, 2, kInter>(m, s);
-  return launch_one<D, 8, 2, kInter>(m, s);
+  if (rows == 32) return launch_one<D, 2, 1, kPlain>(m, s);
+  if (rows == 64) return launch_one<D, 2, 2, kPlain>(m, s);
+  if (rows == 128) return launch_one<D, 4, 2, kPlain>(m, s);
+  return launch_one<D, 8, 2, kPlain>(m, s);
 }
 
 }  // namespace
 
 hipError_t launch_tree_tiles_bf16(int rows, const TreeMfmaArgs& m, hipStream_t s) {
-  const bool il = m.t.a.interleaved != 0;
-  if (m.t.a.D == 128) return il ? launch_rows<128, true>(rows, m, s) : launch_rows<128, false>(rows, m, s);
-  return il ? launch_rows<64, true>(rows, m, s) : launch_rows<64, false>(rows, m, s);
+  const bool plain = !m.t.a.interleaved && !m.t.a.block_positions && !m.t.a.block_valid_mask;
+  if (m.t.a.D == 128) return plain ? launch_rows<128, true>(rows, m, s) : launch_rows<128, false>(rows, m, s);
+  return plain ? launch_rows<64, true>(rows, m, s) : launch_rows<64, false>(rows, m, s);
 }
 
 }  // namespace mepic

@@ -6,9 +6,9 @@
 //   * Work. An item is a tile of kRows rows of one request; its keys come in tiles of 128 slots. The (item, tile) pairs of a KV head form
 //     one sequence that the head's workgroups (one per compute unit, 8 waves) cut into equal runs; a row cut in two
 //     or more goes through partials and tree_merge_kernel, any other is written directly.
-//   * Staging. A thread has one slot and D / 4 dims of it: whole rotary pairs. cos and sin of its slot's position stay in registers and are
-//     turned on by 128 positions from tile to tile (the turn is the same for a wave: scalar registers), found anew every 16 tiles and where
-//     positions jump. K goes to LDS as fp16 in operand order, V as matrix operands too (e4m3 widened to fp16, which holds the codes
+//   * Staging. A wave has eight rotary pairs, a lane one or two slots. cos and sin of its slot's position stay in registers and are
+//     turned on from slot to slot, 64 or 128 positions on (the turn is the same for a wave: scalar registers), found anew every 16 tiles and
+//     where positions jump. K goes to LDS as fp16 in operand order, V as matrix operands too (e4m3 widened to fp16, which holds the codes
 //     exactly); the loads of the next tile are in flight during the products of this one.
 //   * Products. S^T[32 slots x 16 rows] = K Q^T with v_mfma_f32_16x16x32_f16 and O^T[dims x rows] += V^T P^T: a lane owns one row, so
 //     sums, maxima and rescaling are its own. Slots are laid out so that the scores a lane gets are the eight consecutive slots its
@@ -20,6 +20,8 @@
 //     of a row lags by up to 8 (log2 units).
 //   * A marked row, or one that came out Inf or NaN, is computed again by tree_row.
 #pragma once
+#include <type_traits>
+
 #include "lanes.h"
 #include "tree_common.h"
 
@@ -32,8 +34,7 @@ struct TreeLdsTail {  // behind the two tile buffers
   float freq[2][kMaxHalfD];
   uint32_t path[MEPIC_TREE_MAX_NODES][kTreeWords];
   int16_t parent[MEPIC_TREE_MAX_NODES];
-  uint32_t valid[2][4];
-  float scale[2][2][8];  // K and V scale of the tile's blocks (e4m3)
+  int node_pos[MEPIC_TREE_MAX_NODES];
   float ml[8][32][2];
   int bad[256];
   int scan[16];
@@ -61,12 +62,12 @@ __device__ __forceinline__ uint32_t path_bits(const uint32_t* path, int n0, int 
   return s && w + 1 < kTreeWords ? lo | (path[w + 1] << (32 - s)) : lo;
 }
 
-template <bool kFp8, int D, int kGroups, int kTiles, bool kInter>
+template <bool kFp8, int D, int kGroups, int kTiles, bool kPlain>
 __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeMfmaArgs m) {
   constexpr int kRows = kGroups * kTiles * 16, kSlotGroups = 8 / kGroups, kSubs = 4 / kSlotGroups;
   constexpr int kSteps = D / 32, kDims = D / 16;          // products per score, 16-dim tiles of O
   constexpr int E = kFp8 ? 1 : 2, X = 16 / E, DX = D / X;  // bytes per element, elements per granule
-  constexpr int NL = D / 8;                               // rotary pairs per thread: NL low and NL high dims of one slot
+  constexpr int kHalves = D / 64, kTurn = kTreeTile / kHalves;  // slots per thread of a tile, how far apart
   constexpr int kKeyBytes = kTreeTile * D * 2, kTileBytes = 2 * kKeyBytes;
   constexpr int kVGranules = 16 * D * E / 16 / 64;        // 16-byte pieces of V per lane and tile
   constexpr float kKeyFactor = kFp8 ? 1.f : 16.f;
@@ -140,15 +141,16 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
     before = uni(tail.found[1]);
   }
 
-  // ---- what a thread stages: slot `sl` of the tile, pairs of dims of quarter pc (pc is the wave's) ----
-  const int pc = wave >> 1, place = tid & 127;
+  // ---- what a thread stages: the eight pairs of octet pc (the wave's) of slots sl and, D 128, sl + 64; in LDS a slot lies at `place` ----
+  const int pc = D == 128 ? wave : wave & 3, place = D == 128 ? lane : (wave >> 2) * 64 + lane;
   const int sl = (place & ~31) | ((place & 12) << 1) | ((place & 16) >> 2) | (place & 3);
-  float turn_c[NL], turn_s[NL];  // the turn from tile to tile (the same for the wave)
-  auto freq_index = [&](int e) { return kInter ? (e < NL / 2 ? pc * (NL / 2) + e : D / 4 + pc * (NL / 2) + e - NL / 2) : pc * NL + e; };
+  float turn_c[8], turn_s[8];  // the turn by kTurn positions
+  const bool inter = !kPlain && a.interleaved;
+  auto freq_index = [&](int e) { return !inter ? 8 * pc + e : e < 4 ? 4 * pc + e : D / 4 + 4 * pc + e - 4; };
 #pragma unroll
-  for (int e = 0; e < NL; ++e) {
+  for (int e = 0; e < 8; ++e) {
     const int i = freq_index(e);
-    const float f = turns_frac((float)kTreeTile, a.freq_hi[i], a.freq_lo[i]);
+    const float f = turns_frac((float)kTurn, a.freq_hi[i], a.freq_lo[i]);
     turn_c[e] = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(__builtin_amdgcn_cosf(f))));
     turn_s[e] = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(__builtin_amdgcn_sinf(f))));
   }
@@ -183,7 +185,10 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
     const bool nodes_here = t1 * kTreeTile > r.ctx;
     if (nodes_here) {
       const int T = min(r.T, MEPIC_TREE_MAX_NODES);
-      if (tid < T) tail.parent[tid] = (int16_t)tree_parent(ta.parents, r.q0, tid);
+      if (tid < T) {
+        tail.parent[tid] = (int16_t)tree_parent(ta.parents, r.q0, tid);
+        tail.node_pos[tid] = a.q_positions[r.q0 + tid];
+      }
       __syncthreads();
       if (tid < T) {
 #pragma unroll
@@ -202,59 +207,34 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
       }
     }
 
-    // ---- loads of a tile: page ids, positions and masks a tile ahead of the data ----
-    struct Ids { int k_page, v_page, s_page, pos; uint32_t k_mask, v_mask, s_mask, word; float ks, vs; };
-    auto load_ids = [&](int t) {
-      Ids x;
-      const int n = t * kTreeTile + sl, blk = min(n >> logP, a.max_blocks - 1);
-      const int vblk = min(((t * kTreeTile) >> logP) + v_page, a.max_blocks - 1);
-      x.k_page = a.block_tables[bt_row + blk];
-      x.v_page = a.block_tables[bt_row + vblk];
-      x.pos = n;
-      if (n >= r.ctx) x.pos = a.q_positions[min(max(r.q0 + n - r.ctx, 0), a.n_q - 1)];
-      else if (a.block_positions) x.pos = a.block_positions[bt_row + blk] + (n & (P - 1));
-      x.k_mask = x.v_mask = x.s_mask = x.word = ~0u;
-      const int sblk = min(((t * kTreeTile) >> logP) + (tid & 7), a.max_blocks - 1);  // (threads 0 .. 7: the blocks of the tile)
-      if (kFp8) x.s_page = a.block_tables[bt_row + sblk];
-      if (a.block_valid_mask) {
-        x.k_mask = a.block_valid_mask[bt_row + blk];
-        x.v_mask = a.block_valid_mask[bt_row + vblk];
-        if (kFp8) x.s_mask = a.block_valid_mask[bt_row + sblk];
-        if (tid < 4) {  // thread i: the 32 slots of group i
-          const int w0 = min((t * kTreeTile + 32 * tid) >> logP, a.max_blocks - 1);
-          x.word = a.block_valid_mask[bt_row + w0];
-          if (P == 16) x.word = (x.word & 0xffffu) | (a.block_valid_mask[bt_row + min(w0 + 1, a.max_blocks - 1)] << 16);
-        }
-      }
-      x.ks = x.vs = 0.f;
-      return x;
+    // ---- loads of a tile. Block tables, masks and positions come in windows of 64 blocks, a block a lane, two tiles ahead ----
+    auto window = [&](const int32_t* rows, int t) {
+      return rows[bt_row + min((((t * kTreeTile) >> logP) & ~63) + lane, a.max_blocks - 1)];
     };
-    struct Data { uint4 k[kFp8 ? (NL >= 16 ? 2 : 1) : 2 * NL / 8]; uint4 v[kVGranules]; };
-    auto load_data = [&](Data& d, Ids& x, int t) {
-      const size_t pk = (size_t)max(min(x.k_page, a.num_pages - 1), 0) * page_bytes, pv = (size_t)max(min(x.v_page, a.num_pages - 1), 0) * page_bytes;
-      const int s = (t * kTreeTile + sl) & (P - 1);
-      if constexpr (kFp8 && NL == 8) {  // eight low and eight high codes
-        const int c = pc >> 1, o = (pc & 1) * 8;
-        const uint2 lo = *reinterpret_cast<const uint2*>(kp + pk + ((size_t)(c * P + s)) * 16 + o);
-        const uint2 hi = *reinterpret_cast<const uint2*>(kp + pk + ((size_t)((c + DX / 2) * P + s)) * 16 + o);
-        d.k[0] = make_uint4(lo.x, lo.y, hi.x, hi.y);
-      } else {
-        constexpr int kPer = NL / X;  // granules of low dims
+    auto in_window = [&](int t) { return ((t * kTreeTile) >> logP) & 63; };  // the tile's first block in its window
+    auto of_slot = [&](int w, int t, int s) { return __builtin_amdgcn_ds_bpermute(4 * (in_window(t) + (s >> logP)), w); };
+    auto of_block = [&](int w, int t, int blk) { return __builtin_amdgcn_readlane(w, in_window(t) + blk); };
+    auto in_pool = [&](int page) { return (size_t)max(min(page, a.num_pages - 1), 0); };
+    struct Keys { typename std::conditional<kFp8, uint2, uint4>::type lo, hi; };  // eight elements each
+    struct Data { Keys k[kHalves]; uint4 v[kVGranules]; };
+    auto load_data = [&](Data& d, int pages, int t) {
+      const int s = sl & (P - 1);
 #pragma unroll
-        for (int c = 0; c < kPer; ++c) {
-          d.k[c] = *reinterpret_cast<const uint4*>(kp + pk + ((size_t)((pc * kPer + c) * P + s)) * 16);
-          d.k[kPer + c] = *reinterpret_cast<const uint4*>(kp + pk + ((size_t)((DX / 2 + pc * kPer + c) * P + s)) * 16);
+      for (int i = 0; i < kHalves; ++i) {
+        const unsigned char* pk = kp + in_pool(of_slot(pages, t, sl + i * kTurn)) * page_bytes;
+        if constexpr (kFp8) {  // half a granule
+          pk += ((pc >> 1) * P + s) * 16 + (pc & 1) * 8;
+          d.k[i].lo = *reinterpret_cast<const uint2*>(pk);
+          d.k[i].hi = *reinterpret_cast<const uint2*>(pk + DX / 2 * P * 16);
+        } else {
+          pk += (pc * P + s) * 16;
+          d.k[i].lo = *reinterpret_cast<const uint4*>(pk);
+          d.k[i].hi = *reinterpret_cast<const uint4*>(pk + DX / 2 * P * 16);
         }
       }
+      const unsigned char* pv = vp + in_pool(of_block(pages, t, v_page)) * page_bytes + v_first * 16;
 #pragma unroll
-      for (int i = 0; i < kVGranules; ++i) d.v[i] = *reinterpret_cast<const uint4*>(vp + pv + (size_t)(v_first + 64 * i + lane) * 16);
-      if constexpr (kFp8) {
-        if (tid < 8) {
-          const int page = max(min(x.s_page, a.num_pages - 1), 0);
-          x.ks = a.k_scales[page];
-          x.vs = a.v_scales[page];
-        }
-      }
+      for (int i = 0; i < kVGranules; ++i) d.v[i] = *reinterpret_cast<const uint4*>(pv + (64 * i + lane) * 16);
     };
 
     // ---- queries of the wave's rows ----
@@ -292,7 +272,7 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
       for (int kk = 0; kk < kSteps; ++kk)
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          if constexpr (kInter) {
+          if (inter) {
             if (j % 2 == 0) turned(x[kk][j], x[kk][j + 1], 4 * (4 * kk + g) + j / 2);
           } else {
             if (kk < kSteps / 2) turned(x[kk][j], x[kk + kSteps / 2][j], 8 * (4 * kk + g) + j);
@@ -323,97 +303,127 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
     }
     const bool busy = (rg * kTiles) * 16 < n_rows;  // does the wave have rows?
 
-    float cs[NL], sn[NL];
+    float cs[8], sn[8];
     int pos_now = 0;
     Data d;
-    Ids now = load_ids(t0);
-    load_data(d, now, t0);
-    Ids next = load_ids(min(t0 + 1, t1 - 1));
+    const int32_t* masks = kPlain || !a.block_valid_mask ? nullptr : reinterpret_cast<const int32_t*>(a.block_valid_mask);
+    const int32_t* starts = kPlain ? nullptr : a.block_positions;
+    int mask = masks ? window(masks, t0) : -1, start = starts ? window(starts, t0) : 0;  // of tile t, then of the next one
+    const int second = min(t0 + 1, t1 - 1);
+    int pages = window(a.block_tables, t0), mask1 = masks ? window(masks, second) : -1, start1 = starts ? window(starts, second) : 0;
+    load_data(d, pages, t0);
+    float k_scale = 0.f, v_scale = 0.f;
+    if constexpr (kFp8) {
+      k_scale = a.k_scales[in_pool(pages)];
+      v_scale = a.v_scales[in_pool(pages)];
+    }
+    pages = window(a.block_tables, second);
 
+#pragma unroll 1
     for (int t = t0; t < t1; ++t) {
       unsigned char* buf = lds + (t & 1) * kTileBytes;
-      const int n = t * kTreeTile + sl, slots_left = r.kv_len - t * kTreeTile;
+      const int first = t * kTreeTile, slots_left = r.kv_len - first;
       // -- stage tile t --
-      const bool live = n < r.kv_len && ((now.k_mask >> (n & (P - 1))) & 1u);
-      const int pos = n < r.kv_len ? now.pos : pos_now + kTreeTile;
-      const bool on = t != t0 && ((t - t0) & (kReseed - 1)) && __all(pos == pos_now + kTreeTile);
-      pos_now = pos;
-      if (on) {
+      const bool has_nodes = first + kTreeTile > r.ctx;
+      const bool fresh = ((t - t0) & (kReseed - 1)) == 0;
 #pragma unroll
-        for (int e = 0; e < NL; ++e) {
-          const float c = cs[e] * turn_c[e] - sn[e] * turn_s[e];
-          sn[e] = sn[e] * turn_c[e] + cs[e] * turn_s[e];
-          cs[e] = c;
+      for (int i = 0; i < kHalves; ++i) {
+        const int s = sl + i * kTurn, n = first + s;
+        int pos = n;
+        if (starts) pos = of_slot(start, t, s) + (s & (P - 1));
+        if (has_nodes) {
+          if (n >= r.ctx) pos = tail.node_pos[(n - r.ctx) & (MEPIC_TREE_MAX_NODES - 1)];
+          if (n >= r.kv_len) pos = pos_now + kTurn;
         }
-      } else {
+        bool on = !(fresh && i == 0);
+        if (starts || has_nodes) on = on && __all(pos == pos_now + kTurn);
+        pos_now = pos;
+        if (on) {
 #pragma unroll
-        for (int e = 0; e < NL; ++e) {
-          const int i = freq_index(e);
-          const float f = turns_frac((float)pos, a.freq_hi[i], a.freq_lo[i]);
-          cs[e] = kKeyFactor * __builtin_amdgcn_cosf(f);
-          sn[e] = kKeyFactor * __builtin_amdgcn_sinf(f);
-        }
-      }
-      float x[2 * NL];  // low dims, then high ones
-      if constexpr (kFp8) {
+          for (int e = 0; e < 8; ++e) {
+            const float c = cs[e] * turn_c[e] - sn[e] * turn_s[e];
+            sn[e] = sn[e] * turn_c[e] + cs[e] * turn_s[e];
+            cs[e] = c;
+          }
+        } else {
 #pragma unroll
-        for (int c = 0; c < NL / 8; ++c) {
-          const uint32_t w[4] = {d.k[c].x, d.k[c].y, d.k[c].z, d.k[c].w};
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const f32x2 p = __builtin_amdgcn_cvt_pk_f32_fp8(w[j], false), q2 = __builtin_amdgcn_cvt_pk_f32_fp8(w[j], true);
-            x[16 * c + 4 * j] = p[0]; x[16 * c + 4 * j + 1] = p[1]; x[16 * c + 4 * j + 2] = q2[0]; x[16 * c + 4 * j + 3] = q2[1];
+          for (int e = 0; e < 8; ++e) {
+            const int j = freq_index(e);
+            const float f = turns_frac((float)pos, a.freq_hi[j], a.freq_lo[j]);
+            cs[e] = kKeyFactor * __builtin_amdgcn_cosf(f);
+            sn[e] = kKeyFactor * __builtin_amdgcn_sinf(f);
           }
         }
-      } else {
-#pragma unroll
-        for (int c = 0; c < 2 * NL / 8; ++c) {
-          const uint32_t w[4] = {d.k[c].x, d.k[c].y, d.k[c].z, d.k[c].w};
+        float x[16];  // low dims, high dims
+        if constexpr (kFp8) {
+          const uint32_t w[4] = {d.k[i].lo.x, d.k[i].lo.y, d.k[i].hi.x, d.k[i].hi.y};
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            x[8 * c + 2 * j] = __uint_as_float(w[j] << 16);
-            x[8 * c + 2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+            const f32x2 p0 = __builtin_amdgcn_cvt_pk_f32_fp8(w[j], false), p1 = __builtin_amdgcn_cvt_pk_f32_fp8(w[j], true);
+            x[4 * j] = p0[0]; x[4 * j + 1] = p0[1]; x[4 * j + 2] = p1[0]; x[4 * j + 3] = p1[1];
+          }
+        } else {
+          const uint32_t w[8] = {d.k[i].lo.x, d.k[i].lo.y, d.k[i].lo.z, d.k[i].lo.w, d.k[i].hi.x, d.k[i].hi.y, d.k[i].hi.z, d.k[i].hi.w};
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            x[2 * j] = __uint_as_float(w[j] << 16);
+            x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
           }
         }
-      }
+        if (inter) {  // pairs are neighbours: four of the low dims, four of the high ones
 #pragma unroll
-      for (int e = 0; e < NL; ++e) {
-        const int lo = kInter ? 2 * e : e, hi = kInter ? 2 * e + 1 : NL + e;
-        const float y = x[lo] * cs[e] - x[hi] * sn[e];
-        x[hi] = x[hi] * cs[e] + x[lo] * sn[e];
-        x[lo] = y;
-      }
-      Frag kf[2 * NL / 8];
+          for (int e = 0; e < 8; ++e) {
+            const float y = x[2 * e] * cs[e] - x[2 * e + 1] * sn[e];
+            x[2 * e + 1] = x[2 * e + 1] * cs[e] + x[2 * e] * sn[e];
+            x[2 * e] = y;
+          }
+        } else {
 #pragma unroll
-      for (int c = 0; c < 2 * NL / 8; ++c)
+          for (int e = 0; e < 8; ++e) {
+            const float y = x[e] * cs[e] - x[8 + e] * sn[e];
+            x[8 + e] = x[8 + e] * cs[e] + x[e] * sn[e];
+            x[e] = y;
+          }
+        }
+        Frag lo, hi;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) kf[c].w[j] = pack2_f16(x[8 * c + 2 * j], x[8 * c + 2 * j + 1]);
-      if (!__all(live)) {  // slots that take no part may hold anything
+        for (int j = 0; j < 4; ++j) {
+          lo.w[j] = pack2_f16(x[2 * j], x[2 * j + 1]);
+          hi.w[j] = pack2_f16(x[8 + 2 * j], x[9 + 2 * j]);
+        }
+        bool live = n < r.kv_len;
+        if (masks) {
+          const int valid = of_slot(mask, t, s);  // (every lane takes part in the exchange)
+          live = live && ((valid >> (s & (P - 1))) & 1);
+        }
+        if (masks ? !__all(live) : slots_left < kTreeTile) {  // slots that take no part may hold anything
 #pragma unroll
-        for (int c = 0; c < 2 * NL / 8; ++c)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) kf[c].w[j] = live ? kf[c].w[j] : 0u;
-      }
-#pragma unroll
-      for (int c = 0; c < NL / 8; ++c) {
-        *reinterpret_cast<uint4*>(buf + ((pc * (NL / 8) + c) * kTreeTile + place) * 16) = kf[c].u;
-        *reinterpret_cast<uint4*>(buf + ((D / 16 + pc * (NL / 8) + c) * kTreeTile + place) * 16) = kf[NL / 8 + c].u;
+          for (int j = 0; j < 4; ++j) {
+            lo.w[j] = live ? lo.w[j] : 0u;
+            hi.w[j] = live ? hi.w[j] : 0u;
+          }
+        }
+        unsigned char* dst = buf + (pc * kTreeTile + place + i * kTurn) * 16;
+        *reinterpret_cast<uint4*>(dst) = lo.u;
+        *reinterpret_cast<uint4*>(dst + D / 16 * kTreeTile * 16) = hi.u;
+        __builtin_amdgcn_sched_barrier(0);  // (one slot's widened keys in registers at a time)
       }
       // V: a granule is X consecutive slots of one dim, one or two operands of eight
-      const int v_slot = v_page << logP, v_left = slots_left - v_slot;  // slots of the page below kv_len
-      const uint32_t v_bits = now.v_mask & low_bits(v_left);
+      const int v_slot = v_page << logP;
+      uint32_t v_bits = low_bits(slots_left - v_slot);  // of the page's slots those that take part
+      if (masks) v_bits &= (uint32_t)of_block(mask, t, v_page);
       const bool v_whole = (v_bits | ~low_bits(P)) == ~0u;
 #pragma unroll
       for (int i = 0; i < kVGranules; ++i) {
-        const int gi = v_first + 64 * i + lane, per_dim = P / X, dim = gi / per_dim, part = gi % per_dim;
+        const int gi = v_first + 64 * i + lane, log_per = logP - (kFp8 ? 4 : 3), dim = gi >> log_per, part = gi & ((1 << log_per) - 1);
         Frag f[X / 8];
         if constexpr (kFp8) {
           const uint32_t w[4] = {d.v[i].x, d.v[i].y, d.v[i].z, d.v[i].w};
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const f32x2 p = __builtin_amdgcn_cvt_pk_f32_fp8(w[j], false), q2 = __builtin_amdgcn_cvt_pk_f32_fp8(w[j], true);
-            f[j / 2].w[2 * (j & 1)] = pack2_f16(p[0], p[1]);
-            f[j / 2].w[2 * (j & 1) + 1] = pack2_f16(q2[0], q2[1]);
+            const f32x2 p0 = __builtin_amdgcn_cvt_pk_f32_fp8(w[j], false), p1 = __builtin_amdgcn_cvt_pk_f32_fp8(w[j], true);
+            f[j / 2].w[2 * (j & 1)] = pack2_f16(p0[0], p0[1]);
+            f[j / 2].w[2 * (j & 1) + 1] = pack2_f16(p1[0], p1[1]);
           }
         } else {
           f[0].u = d.v[i];
@@ -431,20 +441,21 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
           *reinterpret_cast<uint4*>(buf + kKeyBytes + (octet * D + (dim ^ twist)) * 16) = f[h].u;
         }
       }
-      if (tid < 4) tail.valid[t & 1][tid] = now.word & low_bits(slots_left - 32 * tid);
-      if constexpr (kFp8) {
-        if (tid < 8) {
-          // (a block none of whose slots takes part may have any scale; a K scale of 0 would make NaN of the scores masked later)
-          const bool used = (now.s_mask & low_bits(min(slots_left - (tid << logP), P))) != 0;
-          tail.scale[t & 1][0][tid] = !used ? 1.f : now.ks == 0.f ? 1e-30f : now.ks;
-          tail.scale[t & 1][1][tid] = used ? now.vs : 0.f;
+      const int mask0 = mask;
+      const float ks0 = k_scale, vs0 = v_scale;
+      // -- the next tile's loads, always (the last tile's are its own again): a wait for some of them has to hold on every path --
+      {
+        const int t2 = min(t + 1, t1 - 1), t3 = min(t + 2, t1 - 1);
+        load_data(d, pages, t2);
+        if constexpr (kFp8) {
+          k_scale = a.k_scales[in_pool(pages)];
+          v_scale = a.v_scales[in_pool(pages)];
         }
-      }
-      // -- the next tile's loads --
-      if (t + 1 < t1) {
-        now = next;
-        load_data(d, now, t + 1);
-        next = load_ids(min(t + 2, t1 - 1));
+        mask = mask1;
+        start = start1;
+        pages = window(a.block_tables, t3);
+        if (masks) mask1 = window(masks, t3);
+        if (starts) start1 = window(starts, t3);
       }
       __syncthreads();
 
@@ -452,7 +463,7 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
       if (busy) {
 #pragma unroll 1
         for (int sub = 0; sub < kSubs; ++sub) {
-          const int grp = sg * kSubs + sub, n0 = t * kTreeTile + 32 * grp;
+          const int grp = sg * kSubs + sub, n0 = first + 32 * grp;
           floatx4 s[kTiles][2];
 #pragma unroll
           for (int nr = 0; nr < kTiles; ++nr) s[nr][0] = s[nr][1] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -465,13 +476,27 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
 #pragma unroll
               for (int nr = 0; nr < kTiles; ++nr) s[nr][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k.hv, q[nr][kk].hv, s[nr][h], 0, 0, 0);
             }
-          const uint32_t word = uni(tail.valid[t & 1][grp]);
+          uint32_t word = low_bits(slots_left - 32 * grp);  // slots that take part
+          if (masks)
+            word &= P == 32 ? (uint32_t)of_block(mask0, t, grp)
+                            : ((uint32_t)of_block(mask0, t, 2 * grp) & 0xffffu) | ((uint32_t)of_block(mask0, t, 2 * grp + 1) << 16);
           const bool some = word != ~0u || n0 + 32 > r.ctx;
           float ks = 1.f, ve = 0.f, vm = 1.f, vi = 1.f;  // K scale, V scale = 2^ve vm, vi = 2^-ve
           if constexpr (kFp8) {
-            const int blk = P == 16 ? 2 * grp + (g >> 1) : grp;
-            ks = tail.scale[t & 1][0][blk];
-            const float vs = tail.scale[t & 1][1][blk];
+            auto of = [&](float w, int blk) { return __uint_as_float((uint32_t)of_block((int)__float_as_uint(w), t, blk)); };
+            float vs;
+            if (P == 32) {
+              ks = of(ks0, grp);
+              vs = of(vs0, grp);
+            } else {
+              const float k0 = of(ks0, 2 * grp), k1 = of(ks0, 2 * grp + 1), v0 = of(vs0, 2 * grp), v1 = of(vs0, 2 * grp + 1);
+              ks = g < 2 ? k0 : k1;
+              vs = g < 2 ? v0 : v1;
+            }
+            // (pages none of whose slots takes part may have any scale; a K scale of 0 would make NaN of the scores masked below)
+            const bool used = ((word >> (P == 32 ? 0 : 16 * (g >> 1))) & low_bits(P)) != 0;
+            ks = !used ? 1.f : ks == 0.f ? 1e-30f : ks;
+            vs = used ? vs : 0.f;
             const int e = min(max(__builtin_amdgcn_frexp_expf(vs), -100), 100);
             ve = (float)e;
             vm = ldexpf(vs, -e);
