@@ -20,6 +20,7 @@
 //     of a row lags by up to 8 (log2 units).
 //   * A marked row, or one that came out Inf or NaN, is computed again by tree_row.
 #pragma once
+#include <cstddef>
 #include <type_traits>
 
 #include "lanes.h"
@@ -31,7 +32,7 @@ constexpr int kTreeThreads = 512;
 constexpr int kReseed = 16;  // tiles after which cos and sin are found anew
 
 struct TreeLdsTail {  // behind the two tile buffers
-  float freq[2][kMaxHalfD];
+  TreeArgs args;  // what the loop over tiles does not need is read from here: kernel arguments would fill the scalar registers
   uint32_t path[MEPIC_TREE_MAX_NODES][kTreeWords];
   int16_t parent[MEPIC_TREE_MAX_NODES];
   int node_pos[MEPIC_TREE_MAX_NODES];
@@ -47,6 +48,11 @@ template <int D> constexpr size_t tree_lds_bytes() { return 2 * (size_t)kTreeTil
 __device__ __forceinline__ uint32_t pack2_f16(float lo, float hi) {
   const f32x2 v = {lo, hi};
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2));
+}
+
+// Two e4m3 codes of a word (the low or the high two) as packed fp16, exactly.
+__device__ __forceinline__ uint32_t f16_of_e4m3(uint32_t w, bool high) {
+  return __builtin_bit_cast(uint32_t, high ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, true) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, false));
 }
 
 // The low n bits, n from anything below 0 to anything above 32.
@@ -73,16 +79,23 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
   constexpr float kKeyFactor = kFp8 ? 1.f : 16.f;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   TreeLdsTail& tail = *reinterpret_cast<TreeLdsTail*>(lds + 2 * kTileBytes);
-  const TreeArgs& ta = m.t;
+  const TreeArgs& ta = tail.args;
   const AttnArgs& a = ta.a;
+  const AttnArgs& hot = m.t.a;
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), n16 = lane & 15, g = lane >> 4;
-  const int hk = blockIdx.x % a.Hkv, wg = blockIdx.x / a.Hkv, G = a.G, P = a.P, logP = P == 16 ? 4 : 5;
+  const int hk = blockIdx.x % hot.Hkv, wg = blockIdx.x / hot.Hkv, G = hot.G, P = hot.P, logP = P == 16 ? 4 : 5;
   const int rg = wave % kGroups, sg = wave / kGroups;
 
-  if (tid < D / 2) {
-    tail.freq[0][tid] = a.freq_hi[tid];
-    tail.freq[1][tid] = a.freq_lo[tid];
+  if (tid == 0) {
+    __builtin_memcpy(&tail.args.a, &m.t.a, offsetof(AttnArgs, freq_hi));
+    tail.args.parents = m.t.parents;
+    tail.args.max_q = m.t.max_q;
   }
+  if (tid < D / 2) {
+    tail.args.a.freq_hi[tid] = m.t.a.freq_hi[tid];
+    tail.args.a.freq_lo[tid] = m.t.a.freq_lo[tid];
+  }
+  __syncthreads();
 
   // ---- this workgroup's run: [begin, end) of the (item, tile) pairs of all requests ----
   auto cost_of = [&](int b, int& tiles, int& items) {
@@ -145,7 +158,7 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
   const int pc = D == 128 ? wave : wave & 3, place = D == 128 ? lane : (wave >> 2) * 64 + lane;
   const int sl = (place & ~31) | ((place & 12) << 1) | ((place & 16) >> 2) | (place & 3);
   float turn_c[8], turn_s[8];  // the turn by kTurn positions
-  const bool inter = !kPlain && a.interleaved;
+  const bool inter = !kPlain && hot.interleaved;
   auto freq_index = [&](int e) { return !inter ? 8 * pc + e : e < 4 ? 4 * pc + e : D / 4 + 4 * pc + e - 4; };
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
@@ -155,14 +168,27 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
     turn_s[e] = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(__builtin_amdgcn_sinf(f))));
   }
   const int v_page = wave >> (logP - 4), v_first = (wave & ((P >> 4) - 1)) * (64 * kVGranules);
-  const size_t page_bytes = (size_t)a.Hkv * D * P * E, head_bytes = (size_t)hk * D * P * E;
-  const unsigned char* kp = static_cast<const unsigned char*>(a.k_pages) + head_bytes;
-  const unsigned char* vp = static_cast<const unsigned char*>(a.v_pages) + head_bytes;
+  // a lane's pieces of V: X consecutive slots (part v_part of a page's) of one dim, one or two operands of eight. In LDS operand (octet of
+  // slots, dim) lies at octet * D + (dim ^ twist): lanes that write together, of one dim and several octets, hit different banks
+  const int v_per = P / X, v_part = (v_first + lane) & (v_per - 1), v_dim = (v_first + lane) >> (v_per == 1 ? 0 : v_per == 2 ? 1 : 2);
+  const int v_stride = 64 / v_per * 16;  // (the dims of one lane are multiples of 16 apart: the twist is the same)
+  auto twist_of = [&](int octet) { return P == 16 ? (octet & 1) << 3 : (octet & 3) << 2; };
+  int v_dst[X / 8];
+#pragma unroll
+  for (int h = 0; h < X / 8; ++h) {
+    const int octet = ((v_page << logP) >> 3) + v_part * (X / 8) + h;
+    v_dst[h] = kKeyBytes + (octet * D + (v_dim ^ twist_of(octet))) * 16;
+  }
+  const size_t page_bytes = (size_t)hot.Hkv * D * P * E, head_bytes = (size_t)hk * D * P * E;
+  const unsigned char* kp = static_cast<const unsigned char*>(hot.k_pages) + head_bytes;
+  const unsigned char* vp = static_cast<const unsigned char*>(hot.v_pages) + head_bytes;
 
   while (at < end) {
-    const TreeRequest r = tree_request(a, b);
+    TreeRequest r = tree_request(a, b);
+    r.q0 = uni(r.q0); r.T = uni(r.T); r.kv_len = uni(r.kv_len); r.ctx = uni(r.ctx);
     int tiles, items;
-    const int mine = cost_of(b, tiles, items);
+    const int mine = uni(cost_of(b, tiles, items));
+    tiles = uni(tiles);
     if (at >= before + mine) {  // on to the next request
       before += mine;
       if (++b >= a.B) return;
@@ -209,12 +235,12 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
 
     // ---- loads of a tile. Block tables, masks and positions come in windows of 64 blocks, a block a lane, two tiles ahead ----
     auto window = [&](const int32_t* rows, int t) {
-      return rows[bt_row + min((((t * kTreeTile) >> logP) & ~63) + lane, a.max_blocks - 1)];
+      return rows[bt_row + min((((t * kTreeTile) >> logP) & ~63) + lane, hot.max_blocks - 1)];
     };
     auto in_window = [&](int t) { return ((t * kTreeTile) >> logP) & 63; };  // the tile's first block in its window
     auto of_slot = [&](int w, int t, int s) { return __builtin_amdgcn_ds_bpermute(4 * (in_window(t) + (s >> logP)), w); };
     auto of_block = [&](int w, int t, int blk) { return __builtin_amdgcn_readlane(w, in_window(t) + blk); };
-    auto in_pool = [&](int page) { return (size_t)max(min(page, a.num_pages - 1), 0); };
+    auto in_pool = [&](int page) { return (size_t)max(min(page, hot.num_pages - 1), 0); };
     struct Keys { typename std::conditional<kFp8, uint2, uint4>::type lo, hi; };  // eight elements each
     struct Data { Keys k[kHalves]; uint4 v[kVGranules]; };
     auto load_data = [&](Data& d, int pages, int t) {
@@ -261,7 +287,7 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
         }
       }
       auto turned = [&](float& lo, float& hi, int i) {
-        const float f = turns_frac(pos, tail.freq[0][i], tail.freq[1][i]);
+        const float f = turns_frac(pos, a.freq_hi[i], a.freq_lo[i]);
         const float c = __builtin_amdgcn_cosf(f), s = __builtin_amdgcn_sinf(f);
         const float y = lo * c - hi * s;
         hi = hi * c + lo * s;
@@ -306,24 +332,24 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
     float cs[8], sn[8];
     int pos_now = 0;
     Data d;
-    const int32_t* masks = kPlain || !a.block_valid_mask ? nullptr : reinterpret_cast<const int32_t*>(a.block_valid_mask);
-    const int32_t* starts = kPlain ? nullptr : a.block_positions;
+    const int32_t* masks = kPlain || !hot.block_valid_mask ? nullptr : reinterpret_cast<const int32_t*>(hot.block_valid_mask);
+    const int32_t* starts = kPlain ? nullptr : hot.block_positions;
     int mask = masks ? window(masks, t0) : -1, start = starts ? window(starts, t0) : 0;  // of tile t, then of the next one
     const int second = min(t0 + 1, t1 - 1);
-    int pages = window(a.block_tables, t0), mask1 = masks ? window(masks, second) : -1, start1 = starts ? window(starts, second) : 0;
+    int pages = window(hot.block_tables, t0), mask1 = masks ? window(masks, second) : -1, start1 = starts ? window(starts, second) : 0;
     load_data(d, pages, t0);
     float k_scale = 0.f, v_scale = 0.f;
     if constexpr (kFp8) {
-      k_scale = a.k_scales[in_pool(pages)];
-      v_scale = a.v_scales[in_pool(pages)];
+      k_scale = hot.k_scales[in_pool(pages)];
+      v_scale = hot.v_scales[in_pool(pages)];
     }
-    pages = window(a.block_tables, second);
+    pages = window(hot.block_tables, second);
 
-#pragma unroll 1
-    for (int t = t0; t < t1; ++t) {
+    int mask_used = -1;  // what the products of the last staged tile need
+    float ks_used = 0.f, vs_used = 0.f;
+    auto stage = [&](int t) {  // tile t into its buffer, and the loads of tile t + 1
       unsigned char* buf = lds + (t & 1) * kTileBytes;
       const int first = t * kTreeTile, slots_left = r.kv_len - first;
-      // -- stage tile t --
       const bool has_nodes = first + kTreeTile > r.ctx;
       const bool fresh = ((t - t0) & (kReseed - 1)) == 0;
 #pragma unroll
@@ -341,9 +367,10 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
         if (on) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const float c = cs[e] * turn_c[e] - sn[e] * turn_s[e];
-            sn[e] = sn[e] * turn_c[e] + cs[e] * turn_s[e];
-            cs[e] = c;
+            const float y = sn[e] * turn_s[e];  // (in this order in place: no register is copied)
+            sn[e] *= turn_c[e];
+            sn[e] = __builtin_fmaf(cs[e], turn_s[e], sn[e]);
+            cs[e] = __builtin_fmaf(cs[e], turn_c[e], -y);
           }
         } else {
 #pragma unroll
@@ -397,6 +424,7 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
           live = live && ((valid >> (s & (P - 1))) & 1);
         }
         if (masks ? !__all(live) : slots_left < kTreeTile) {  // slots that take no part may hold anything
+          asm volatile("");  // (a branch, not eight selects in every tile)
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             lo.w[j] = live ? lo.w[j] : 0u;
@@ -408,165 +436,176 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
         *reinterpret_cast<uint4*>(dst + D / 16 * kTreeTile * 16) = hi.u;
         __builtin_amdgcn_sched_barrier(0);  // (one slot's widened keys in registers at a time)
       }
-      // V: a granule is X consecutive slots of one dim, one or two operands of eight
       const int v_slot = v_page << logP;
       uint32_t v_bits = low_bits(slots_left - v_slot);  // of the page's slots those that take part
       if (masks) v_bits &= (uint32_t)of_block(mask, t, v_page);
       const bool v_whole = (v_bits | ~low_bits(P)) == ~0u;
 #pragma unroll
       for (int i = 0; i < kVGranules; ++i) {
-        const int gi = v_first + 64 * i + lane, log_per = logP - (kFp8 ? 4 : 3), dim = gi >> log_per, part = gi & ((1 << log_per) - 1);
         Frag f[X / 8];
         if constexpr (kFp8) {
           const uint32_t w[4] = {d.v[i].x, d.v[i].y, d.v[i].z, d.v[i].w};
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const f32x2 p0 = __builtin_amdgcn_cvt_pk_f32_fp8(w[j], false), p1 = __builtin_amdgcn_cvt_pk_f32_fp8(w[j], true);
-            f[j / 2].w[2 * (j & 1)] = pack2_f16(p0[0], p0[1]);
-            f[j / 2].w[2 * (j & 1) + 1] = pack2_f16(p1[0], p1[1]);
+            f[j / 2].w[2 * (j & 1)] = f16_of_e4m3(w[j], false);
+            f[j / 2].w[2 * (j & 1) + 1] = f16_of_e4m3(w[j], true);
           }
         } else {
           f[0].u = d.v[i];
         }
 #pragma unroll
         for (int h = 0; h < X / 8; ++h) {
-          const int oct = part * (X / 8) + h;  // of the page
           if (!v_whole) {
-            const uint32_t keep = v_bits >> (8 * oct);
+            asm volatile("");
+            const uint32_t keep = v_bits >> (8 * (v_part * (X / 8) + h));
 #pragma unroll
             for (int j = 0; j < 4; ++j)
               f[h].w[j] &= ((keep >> (2 * j)) & 1u ? 0x0000ffffu : 0u) | ((keep >> (2 * j + 1)) & 1u ? 0xffff0000u : 0u);
           }
-          const int octet = (v_slot >> 3) + oct, twist = P == 16 ? (octet & 1) << 3 : (octet & 3) << 2;
-          *reinterpret_cast<uint4*>(buf + kKeyBytes + (octet * D + (dim ^ twist)) * 16) = f[h].u;
+          *reinterpret_cast<uint4*>(buf + v_dst[h] + i * v_stride) = f[h].u;
         }
       }
-      const int mask0 = mask;
-      const float ks0 = k_scale, vs0 = v_scale;
-      // -- the next tile's loads, always (the last tile's are its own again): a wait for some of them has to hold on every path --
+      mask_used = mask;
+      ks_used = k_scale;
+      vs_used = v_scale;
+      // the loads always (the last tile's are its own again): a wait for some of them has to hold on every path
       {
         const int t2 = min(t + 1, t1 - 1), t3 = min(t + 2, t1 - 1);
         load_data(d, pages, t2);
         if constexpr (kFp8) {
-          k_scale = a.k_scales[in_pool(pages)];
-          v_scale = a.v_scales[in_pool(pages)];
+          k_scale = hot.k_scales[in_pool(pages)];
+          v_scale = hot.v_scales[in_pool(pages)];
         }
         mask = mask1;
         start = start1;
-        pages = window(a.block_tables, t3);
+        pages = window(hot.block_tables, t3);
         if (masks) mask1 = window(masks, t3);
         if (starts) start1 = window(starts, t3);
       }
-      __syncthreads();
-
-      // -- products --
-      if (busy) {
+    };
+    auto products = [&](int t, int mask0, float ks0, float vs0) {
+      const unsigned char* buf = lds + (t & 1) * kTileBytes;
+      const int first = t * kTreeTile, slots_left = r.kv_len - first;
 #pragma unroll 1
-        for (int sub = 0; sub < kSubs; ++sub) {
-          const int grp = sg * kSubs + sub, n0 = first + 32 * grp;
-          floatx4 s[kTiles][2];
+      for (int sub = 0; sub < kSubs; ++sub) {
+        const int grp = sg * kSubs + sub, n0 = first + 32 * grp;
+        floatx4 s[kTiles][2];
 #pragma unroll
-          for (int nr = 0; nr < kTiles; ++nr) s[nr][0] = s[nr][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+        for (int nr = 0; nr < kTiles; ++nr) s[nr][0] = s[nr][1] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int kk = 0; kk < kSteps; ++kk)
+        for (int kk = 0; kk < kSteps; ++kk)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              Frag k;
-              k.u = *reinterpret_cast<const uint4*>(buf + ((4 * kk + g) * kTreeTile + 32 * grp + 16 * h + n16) * 16);
+          for (int h = 0; h < 2; ++h) {
+            Frag k;
+            k.u = *reinterpret_cast<const uint4*>(buf + ((4 * kk + g) * kTreeTile + 32 * grp + 16 * h + n16) * 16);
 #pragma unroll
-              for (int nr = 0; nr < kTiles; ++nr) s[nr][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k.hv, q[nr][kk].hv, s[nr][h], 0, 0, 0);
-            }
-          uint32_t word = low_bits(slots_left - 32 * grp);  // slots that take part
-          if (masks)
-            word &= P == 32 ? (uint32_t)of_block(mask0, t, grp)
-                            : ((uint32_t)of_block(mask0, t, 2 * grp) & 0xffffu) | ((uint32_t)of_block(mask0, t, 2 * grp + 1) << 16);
-          const bool some = word != ~0u || n0 + 32 > r.ctx;
-          float ks = 1.f, ve = 0.f, vm = 1.f, vi = 1.f;  // K scale, V scale = 2^ve vm, vi = 2^-ve
-          if constexpr (kFp8) {
-            auto of = [&](float w, int blk) { return __uint_as_float((uint32_t)of_block((int)__float_as_uint(w), t, blk)); };
-            float vs;
-            if (P == 32) {
-              ks = of(ks0, grp);
-              vs = of(vs0, grp);
-            } else {
-              const float k0 = of(ks0, 2 * grp), k1 = of(ks0, 2 * grp + 1), v0 = of(vs0, 2 * grp), v1 = of(vs0, 2 * grp + 1);
-              ks = g < 2 ? k0 : k1;
-              vs = g < 2 ? v0 : v1;
-            }
-            // (pages none of whose slots takes part may have any scale; a K scale of 0 would make NaN of the scores masked below)
-            const bool used = ((word >> (P == 32 ? 0 : 16 * (g >> 1))) & low_bits(P)) != 0;
-            ks = !used ? 1.f : ks == 0.f ? 1e-30f : ks;
-            vs = used ? vs : 0.f;
-            const int e = min(max(__builtin_amdgcn_frexp_expf(vs), -100), 100);
-            ve = (float)e;
-            vm = ldexpf(vs, -e);
-            vi = ldexpf(1.f, -e);
+            for (int nr = 0; nr < kTiles; ++nr) s[nr][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k.hv, q[nr][kk].hv, s[nr][h], 0, 0, 0);
           }
-          Frag p[kTiles];
+        uint32_t word = low_bits(slots_left - 32 * grp);  // slots that take part
+        if (masks)
+          word &= P == 32 ? (uint32_t)of_block(mask0, t, grp)
+                          : ((uint32_t)of_block(mask0, t, 2 * grp) & 0xffffu) | ((uint32_t)of_block(mask0, t, 2 * grp + 1) << 16);
+        const bool some = word != ~0u || n0 + 32 > r.ctx;
+        float ks = 1.f, ve = 0.f, vm = 1.f, vi = 1.f;  // K scale, V scale = 2^ve vm, vi = 2^-ve
+        if constexpr (kFp8) {
+          auto of = [&](float w, int blk) { return __uint_as_float((uint32_t)of_block((int)__float_as_uint(w), t, blk)); };
+          float vs;
+          if (P == 32) {
+            ks = of(ks0, grp);
+            vs = of(vs0, grp);
+          } else {
+            const float k0 = of(ks0, 2 * grp), k1 = of(ks0, 2 * grp + 1), v0 = of(vs0, 2 * grp), v1 = of(vs0, 2 * grp + 1);
+            ks = g < 2 ? k0 : k1;
+            vs = g < 2 ? v0 : v1;
+          }
+          // (pages none of whose slots takes part may have any scale; a K scale of 0 would make NaN of the scores masked below)
+          const bool used = ((word >> (P == 32 ? 0 : 16 * (g >> 1))) & low_bits(P)) != 0;
+          ks = !used ? 1.f : ks == 0.f ? 1e-30f : ks;
+          vs = used ? vs : 0.f;
+          const int e = min(max(__builtin_amdgcn_frexp_expf(vs), -100), 100);
+          ve = (float)e;
+          vm = ldexpf(vs, -e);
+          vi = ldexpf(1.f, -e);
+        }
+        Frag p[kTiles];
+#pragma unroll
+        for (int nr = 0; nr < kTiles; ++nr) {
+          float y[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) y[j] = s[nr][j >> 2][j & 3];
+          if constexpr (!kFp8) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) least[nr] = fminf(least[nr], y[j]);
+          }
+          if (some) {
+            const uint32_t bits = (word & path_bits(tail.path[row_node[nr]], n0, r.ctx)) >> (8 * g);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = (bits >> j) & 1u ? y[j] : -INFINITY;
+          }
+          const float c = row_scale[nr] * ks;
+          float most = y[0];
+#pragma unroll
+          for (int j = 1; j < 8; ++j) most = fmaxf(most, y[j]);
+          most = most == -INFINITY ? most : __builtin_fmaf(most, c, ve);
+          if (__any(most > top[nr] + 8.f)) {
+            const float now_top = fmaxf(top[nr], max_over_kgroups(most));
+            const float f = now_top == top[nr] ? 1.f : __builtin_amdgcn_exp2f(top[nr] - now_top);
+            top[nr] = now_top;
+            ref[nr] = now_top == -INFINITY ? 0.f : now_top;
+            sum[nr] *= f;
+#pragma unroll
+            for (int dt = 0; dt < kDims; ++dt)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) o[nr][dt][i] *= f;
+          }
+          const float shift = ve - ref[nr];
+          float part = 0.f;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            y[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(y[j], c, shift));
+            part += y[j];
+          }
+          if constexpr (kFp8) {
+            sum[nr] = __builtin_fmaf(part, vi, sum[nr]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) p[nr].w[j] = pack2_f16(y[2 * j] * vm, y[2 * j + 1] * vm);
+          } else {
+            sum[nr] += part;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) p[nr].w[j] = pack2_bf16(y[2 * j], y[2 * j + 1]);
+          }
+        }
+        const int twist = twist_of(g);
+#pragma unroll
+        for (int dt = 0; dt < kDims; ++dt) {
+          Frag v;
+          v.u = *reinterpret_cast<const uint4*>(buf + kKeyBytes + ((4 * grp + g) * D + ((16 * dt + n16) ^ twist)) * 16);
 #pragma unroll
           for (int nr = 0; nr < kTiles; ++nr) {
-            float y[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] = s[nr][j >> 2][j & 3];
-            if constexpr (!kFp8) {
-#pragma unroll
-              for (int j = 0; j < 8; ++j) least[nr] = fminf(least[nr], y[j]);
-            }
-            if (some) {
-              const uint32_t bits = (word & path_bits(tail.path[row_node[nr]], n0, r.ctx)) >> (8 * g);
-#pragma unroll
-              for (int j = 0; j < 8; ++j) y[j] = (bits >> j) & 1u ? y[j] : -INFINITY;
-            }
-            const float c = row_scale[nr] * ks;
-            float most = y[0];
-#pragma unroll
-            for (int j = 1; j < 8; ++j) most = fmaxf(most, y[j]);
-            most = most == -INFINITY ? most : __builtin_fmaf(most, c, ve);
-            if (__any(most > top[nr] + 8.f)) {
-              const float now_top = fmaxf(top[nr], max_over_kgroups(most));
-              const float f = now_top == top[nr] ? 1.f : __builtin_amdgcn_exp2f(top[nr] - now_top);
-              top[nr] = now_top;
-              ref[nr] = now_top == -INFINITY ? 0.f : now_top;
-              sum[nr] *= f;
-#pragma unroll
-              for (int dt = 0; dt < kDims; ++dt)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) o[nr][dt][i] *= f;
-            }
-            const float shift = ve - ref[nr];
-            float part = 0.f;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              y[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(y[j], c, shift));
-              part += y[j];
-            }
-            if constexpr (kFp8) {
-              sum[nr] = __builtin_fmaf(part, vi, sum[nr]);
-#pragma unroll
-              for (int j = 0; j < 4; ++j) p[nr].w[j] = pack2_f16(y[2 * j] * vm, y[2 * j + 1] * vm);
-            } else {
-              sum[nr] += part;
-#pragma unroll
-              for (int j = 0; j < 4; ++j) p[nr].w[j] = pack2_bf16(y[2 * j], y[2 * j + 1]);
-            }
-          }
-          const int twist = P == 16 ? (g & 1) << 3 : g << 2;
-#pragma unroll
-          for (int dt = 0; dt < kDims; ++dt) {
-            Frag v;
-            v.u = *reinterpret_cast<const uint4*>(buf + kKeyBytes + ((4 * grp + g) * D + ((16 * dt + n16) ^ twist)) * 16);
-#pragma unroll
-            for (int nr = 0; nr < kTiles; ++nr) {
-              if constexpr (kFp8) o[nr][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v.hv, p[nr].hv, o[nr][dt], 0, 0, 0);
-              else o[nr][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.v, p[nr].v, o[nr][dt], 0, 0, 0);
-            }
+            if constexpr (kFp8) o[nr][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v.hv, p[nr].hv, o[nr][dt], 0, 0, 0);
+            else o[nr][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.v, p[nr].v, o[nr][dt], 0, 0, 0);
           }
         }
       }
+    };
+
+    // Of a SIMD's two waves one stages a tile before the products of the one in front, the other after them: vector and matrix
+    // instructions of the two meet.
+    const bool early = wave < 4;
+    stage(t0);
+    __syncthreads();
+#pragma unroll 1
+    for (int t = t0; t < t1; ++t) {
+      const int mask0 = mask_used;
+      const float ks0 = ks_used, vs0 = vs_used;
+      const bool more = t + 1 < t1;
+      if (early && more) stage(t + 1);
+      if (busy) products(t, mask0, ks0, vs0);
+      if (!early && more) stage(t + 1);
+      __syncthreads();
     }
 
     // ---- the waves of a group of rows merged, rows written ----
-    __syncthreads();  // (the last tile's operands are read)
     const int rows_here = min(n_rows, kRows);
     if (busy) {
 #pragma unroll
