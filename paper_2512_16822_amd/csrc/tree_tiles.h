@@ -76,6 +76,7 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
   constexpr int kHalves = D / 64, kTurn = kTreeTile / kHalves;  // slots per thread of a tile, how far apart
   constexpr int kKeyBytes = kTreeTile * D * 2, kTileBytes = 2 * kKeyBytes;
   constexpr int kVGranules = 16 * D * E / 16 / 64;        // 16-byte pieces of V per lane and tile
+  constexpr int kRing = kTiles == 1 && D == 128 ? 8 : 4;  // operands in flight: some 150 clocks a read, 16 a product
   constexpr float kKeyFactor = kFp8 ? 1.f : 16.f;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   TreeLdsTail& tail = *reinterpret_cast<TreeLdsTail*>(lds + 2 * kTileBytes);
@@ -179,6 +180,7 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
     const int octet = ((v_page << logP) >> 3) + v_part * (X / 8) + h;
     v_dst[h] = kKeyBytes + (octet * D + (v_dim ^ twist_of(octet))) * 16;
   }
+  const int k_src = (g * kTreeTile + n16) * 16, v_src = kKeyBytes + (g * D + (n16 ^ twist_of(g))) * 16;  // a lane's first operands
   const size_t page_bytes = (size_t)hot.Hkv * D * P * E, head_bytes = (size_t)hk * D * P * E;
   const unsigned char* kp = static_cast<const unsigned char*>(hot.k_pages) + head_bytes;
   const unsigned char* vp = static_cast<const unsigned char*>(hot.v_pages) + head_bytes;
@@ -492,15 +494,28 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
         floatx4 s[kTiles][2];
 #pragma unroll
         for (int nr = 0; nr < kTiles; ++nr) s[nr][0] = s[nr][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+        // Operands come through a ring of kRing registers sets, each read right behind the product that frees its place; the order is
+        // pinned (left to itself the compiler waits for each read before it requests the next).
+        Frag k[kRing];
+        auto k_at = [&](int i) { return *reinterpret_cast<const uint4*>(buf + k_src + grp * 512 + (4 * (i >> 1) * kTreeTile + 16 * (i & 1)) * 16); };
 #pragma unroll
-        for (int kk = 0; kk < kSteps; ++kk)
+        for (int i = 0; i < kRing; ++i) k[i].u = k_at(i);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            Frag k;
-            k.u = *reinterpret_cast<const uint4*>(buf + ((4 * kk + g) * kTreeTile + 32 * grp + 16 * h + n16) * 16);
+        for (int i = 0; i < 2 * kSteps; ++i) {
 #pragma unroll
-            for (int nr = 0; nr < kTiles; ++nr) s[nr][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k.hv, q[nr][kk].hv, s[nr][h], 0, 0, 0);
+          for (int nr = 0; nr < kTiles; ++nr) s[nr][i & 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k[i % kRing].hv, q[nr][i >> 1].hv, s[nr][i & 1], 0, 0, 0);
+          if (i + kRing < 2 * kSteps) {
+            k[i % kRing].u = k_at(i + kRing);
+            __builtin_amdgcn_sched_barrier(0);
           }
+        }
+        Frag v[kRing];
+        auto v_at = [&](int dt) { return *reinterpret_cast<const uint4*>(buf + v_src + grp * (4 * D * 16) + dt * 256); };
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < kRing && i < kDims; ++i) v[i].u = v_at(i);
+        __builtin_amdgcn_sched_barrier(0);
         uint32_t word = low_bits(slots_left - 32 * grp);  // slots that take part
         if (masks)
           word &= P == 32 ? (uint32_t)of_block(mask0, t, grp)
@@ -575,15 +590,17 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
             for (int j = 0; j < 4; ++j) p[nr].w[j] = pack2_bf16(y[2 * j], y[2 * j + 1]);
           }
         }
-        const int twist = twist_of(g);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int dt = 0; dt < kDims; ++dt) {
-          Frag v;
-          v.u = *reinterpret_cast<const uint4*>(buf + kKeyBytes + ((4 * grp + g) * D + ((16 * dt + n16) ^ twist)) * 16);
 #pragma unroll
           for (int nr = 0; nr < kTiles; ++nr) {
-            if constexpr (kFp8) o[nr][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v.hv, p[nr].hv, o[nr][dt], 0, 0, 0);
-            else o[nr][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.v, p[nr].v, o[nr][dt], 0, 0, 0);
+            if constexpr (kFp8) o[nr][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[dt % kRing].hv, p[nr].hv, o[nr][dt], 0, 0, 0);
+            else o[nr][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[dt % kRing].v, p[nr].v, o[nr][dt], 0, 0, 0);
+          }
+          if (dt + kRing < kDims) {
+            v[dt % kRing].u = v_at(dt + kRing);
+            __builtin_amdgcn_sched_barrier(0);
           }
         }
       }
