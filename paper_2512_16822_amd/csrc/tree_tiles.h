@@ -245,11 +245,11 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
     auto in_pool = [&](int page) { return (size_t)max(min(page, hot.num_pages - 1), 0); };
     struct Keys { typename std::conditional<kFp8, uint2, uint4>::type lo, hi; };  // eight elements each
     struct Data { Keys k[kHalves]; uint4 v[kVGranules]; };
-    auto load_data = [&](Data& d, int pages, int t) {
+    auto load_k = [&](Data& d, const int (&page)[kHalves]) {
       const int s = sl & (P - 1);
 #pragma unroll
       for (int i = 0; i < kHalves; ++i) {
-        const unsigned char* pk = kp + in_pool(of_slot(pages, t, sl + i * kTurn)) * page_bytes;
+        const unsigned char* pk = kp + in_pool(page[i]) * page_bytes;
         if constexpr (kFp8) {  // half a granule
           pk += ((pc >> 1) * P + s) * 16 + (pc & 1) * 8;
           d.k[i].lo = *reinterpret_cast<const uint2*>(pk);
@@ -260,6 +260,8 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
           d.k[i].hi = *reinterpret_cast<const uint4*>(pk + DX / 2 * P * 16);
         }
       }
+    };
+    auto load_v = [&](Data& d, int pages, int t) {
       const unsigned char* pv = vp + in_pool(of_block(pages, t, v_page)) * page_bytes + v_first * 16;
 #pragma unroll
       for (int i = 0; i < kVGranules; ++i) d.v[i] = *reinterpret_cast<const uint4*>(pv + (64 * i + lane) * 16);
@@ -339,7 +341,11 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
     int mask = masks ? window(masks, t0) : -1, start = starts ? window(starts, t0) : 0;  // of tile t, then of the next one
     const int second = min(t0 + 1, t1 - 1);
     int pages = window(hot.block_tables, t0), mask1 = masks ? window(masks, second) : -1, start1 = starts ? window(starts, second) : 0;
-    load_data(d, pages, t0);
+    int k_page[kHalves];
+#pragma unroll
+    for (int i = 0; i < kHalves; ++i) k_page[i] = of_slot(pages, t0, sl + i * kTurn);
+    load_k(d, k_page);
+    load_v(d, pages, t0);
     float k_scale = 0.f, v_scale = 0.f;
     if constexpr (kFp8) {
       k_scale = hot.k_scales[in_pool(pages)];
@@ -354,6 +360,11 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
       const int first = t * kTreeTile, slots_left = r.kv_len - first;
       const bool has_nodes = first + kTreeTile > r.ctx;
       const bool fresh = ((t - t0) & (kReseed - 1)) == 0;
+      // (loads always, the last tile's are its own again: a wait for some of them has to hold on every path. The exchange of page ids comes
+      // before the writes to LDS: behind them it waits for them.)
+      const int t2 = min(t + 1, t1 - 1), t3 = min(t + 2, t1 - 1);
+#pragma unroll
+      for (int i = 0; i < kHalves; ++i) k_page[i] = of_slot(pages, t2, sl + i * kTurn);
 #pragma unroll
       for (int i = 0; i < kHalves; ++i) {
         const int s = sl + i * kTurn, n = first + s;
@@ -438,6 +449,7 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
         *reinterpret_cast<uint4*>(dst + D / 16 * kTreeTile * 16) = hi.u;
         __builtin_amdgcn_sched_barrier(0);  // (one slot's widened keys in registers at a time)
       }
+      load_k(d, k_page);
       const int v_slot = v_page << logP;
       uint32_t v_bits = low_bits(slots_left - v_slot);  // of the page's slots those that take part
       if (masks) v_bits &= (uint32_t)of_block(mask, t, v_page);
@@ -470,20 +482,16 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
       mask_used = mask;
       ks_used = k_scale;
       vs_used = v_scale;
-      // the loads always (the last tile's are its own again): a wait for some of them has to hold on every path
-      {
-        const int t2 = min(t + 1, t1 - 1), t3 = min(t + 2, t1 - 1);
-        load_data(d, pages, t2);
-        if constexpr (kFp8) {
-          k_scale = hot.k_scales[in_pool(pages)];
-          v_scale = hot.v_scales[in_pool(pages)];
-        }
-        mask = mask1;
-        start = start1;
-        pages = window(hot.block_tables, t3);
-        if (masks) mask1 = window(masks, t3);
-        if (starts) start1 = window(starts, t3);
+      load_v(d, pages, t2);
+      if constexpr (kFp8) {
+        k_scale = hot.k_scales[in_pool(pages)];
+        v_scale = hot.v_scales[in_pool(pages)];
       }
+      mask = mask1;
+      start = start1;
+      pages = window(hot.block_tables, t3);
+      if (masks) mask1 = window(masks, t3);
+      if (starts) start1 = window(starts, t3);
     };
     auto products = [&](int t, int mask0, float ks0, float vs0) {
       const unsigned char* buf = lds + (t & 1) * kTileBytes;
