@@ -31,10 +31,18 @@ def _rotate(x, pos, theta, interleaved):
     return out
 
 
+def _lengths(x, interleaved):
+    """The length of each rotary pair of x [..., D]."""
+    D = x.shape[-1]
+    a, b = (x[..., 0::2], x[..., 1::2]) if interleaved else (x[..., : D // 2], x[..., D // 2:])
+    return np.sqrt(a * a + b * b)
+
+
 def tree_attention(q, k_pages, v_pages, block_tables, kv_lens, q_positions, cu_q_lens, parents, *, theta, k_scales=None, v_scales=None,
                    block_positions=None, block_valid_mask=None, sm_scale=0.0, interleaved=False):
     """q [n, Hq, D], k_pages [N, Hkv, D/X, P, X], v_pages [N, Hkv, D, P] in float64. parents: [n] or None (chains).
-    Returns out [n, Hq, D], the weighted mean of |v| [n, Hq, D], and the largest scale * sum |q_i k_i| a row sees [n, Hq]."""
+    Returns out [n, Hq, D], the weighted mean of |v| [n, Hq, D], and [n, Hq] the largest scale * sum over rotary pairs of the product of
+    the query's and the key's length in the pair that a row sees (no rotation changes these lengths)."""
     n_q, Hq, D = q.shape
     Hkv, P = k_pages.shape[1], v_pages.shape[3]
     G, scale = Hq // Hkv, sm_scale if sm_scale > 0 else D ** -0.5
@@ -72,7 +80,7 @@ def tree_attention(q, k_pages, v_pages, block_tables, kv_lens, q_positions, cu_q
                 w /= w.sum()
                 out[q0 + i, h] = w @ vs[:, h // G]
                 mean[q0 + i, h] = w @ np.abs(vs[:, h // G])
-                size[q0 + i, h] = scale * (np.abs(ks[:, h // G]) @ np.abs(qr[i, h])).max()
+                size[q0 + i, h] = scale * (_lengths(ks[:, h // G], interleaved) @ _lengths(qr[i, h], interleaved)).max()
     return out, mean, size
 
 

@@ -36,6 +36,7 @@ struct TreeLdsTail {  // behind the two tile buffers
   uint32_t path[MEPIC_TREE_MAX_NODES][kTreeWords];
   int16_t parent[MEPIC_TREE_MAX_NODES];
   int node_pos[MEPIC_TREE_MAX_NODES];
+  float2 back[kMaxHalfD];  // cos and sin of a window's turn
   float ml[8][32][2];
   int bad[256];
   int scan[16];
@@ -77,7 +78,8 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
   constexpr int kKeyBytes = kTreeTile * D * 2, kTileBytes = 2 * kKeyBytes;
   constexpr int kVGranules = 16 * D * E / 16 / 64;        // 16-byte pieces of V per lane and tile
   constexpr int kRing = kTiles == 1 && D == 128 ? 8 : 4;  // operands in flight: some 150 clocks a read, 16 a product
-  constexpr float kKeyFactor = kFp8 ? 1.f : 16.f;
+  constexpr bool kWindows = kPlain && kTiles == 1;  // keys turned from the start of a window of two tiles (see Staging)
+  constexpr float kKeyFactor = kFp8 || kWindows ? 1.f : 16.f;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   TreeLdsTail& tail = *reinterpret_cast<TreeLdsTail*>(lds + 2 * kTileBytes);
   const TreeArgs& ta = tail.args;
@@ -95,6 +97,10 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
   if (tid < D / 2) {
     tail.args.a.freq_hi[tid] = m.t.a.freq_hi[tid];
     tail.args.a.freq_lo[tid] = m.t.a.freq_lo[tid];
+    if (kWindows) {
+      const float f = turns_frac(2.f * kTreeTile, m.t.a.freq_hi[tid], m.t.a.freq_lo[tid]);
+      tail.back[tid] = make_float2(__builtin_amdgcn_cosf(f), __builtin_amdgcn_sinf(f));
+    }
   }
   __syncthreads();
 
@@ -168,6 +174,33 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
     turn_c[e] = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(__builtin_amdgcn_cosf(f))));
     turn_s[e] = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(__builtin_amdgcn_sinf(f))));
   }
+  // kWindows: cos and sin of a thread's slots of a window, for two pairs a register
+  f16x2 win_c[kWindows ? 2 * kHalves : 1][4], win_s[kWindows ? 2 * kHalves : 1][4];
+  bool win_kept = false;
+  auto keep_window = [&]() {
+    float c[8], s[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float f = turns_frac((float)sl, a.freq_hi[freq_index(e)], a.freq_lo[freq_index(e)]);
+      c[e] = __builtin_amdgcn_cosf(f);
+      s[e] = __builtin_amdgcn_sinf(f);
+    }
+#pragma unroll
+    for (int h = 0; h < (kWindows ? 2 * kHalves : 1); ++h) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        win_c[h][j] = __builtin_bit_cast(f16x2, pack2_f16(c[2 * j], c[2 * j + 1]));
+        win_s[h][j] = __builtin_bit_cast(f16x2, pack2_f16(s[2 * j], s[2 * j + 1]));
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float y = c[e] * turn_c[e] - s[e] * turn_s[e];
+        s[e] = s[e] * turn_c[e] + c[e] * turn_s[e];
+        c[e] = y;
+      }
+    }
+    win_kept = true;
+  };
   const int v_page = wave >> (logP - 4), v_first = (wave & ((P >> 4) - 1)) * (64 * kVGranules);
   // a lane's pieces of V: X consecutive slots (part v_part of a page's) of one dim, one or two operands of eight. In LDS operand (octet of
   // slots, dim) lies at octet * D + (dim ^ twist): lanes that write together, of one dim and several octets, hit different banks
@@ -268,7 +301,9 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
     };
 
     // ---- queries of the wave's rows ----
+    const int base = kWindows ? t0 * kTreeTile : 0;  // positions are counted from here
     Frag q[kTiles][kSteps];
+    float turned_q[kWindows ? kSteps : 1][8];
     float row_scale[kTiles];
     int row_node[kTiles];
 #pragma unroll
@@ -278,7 +313,7 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
       row_node[nr] = there ? min(node, MEPIC_TREE_MAX_NODES - 1) : 0;
       float x[kSteps][8];
       const uint16_t* src = static_cast<const uint16_t*>(a.q) + ((size_t)(r.q0 + row_node[nr]) * a.Hq + (size_t)hk * G + head) * D;
-      const float pos = there ? (float)a.q_positions[r.q0 + row_node[nr]] : 0.f;
+      const float pos = there ? (float)(int)((uint32_t)a.q_positions[r.q0 + row_node[nr]] - (uint32_t)base) : 0.f;
 #pragma unroll
       for (int kk = 0; kk < kSteps; ++kk) {
         uint4 u = make_uint4(0, 0, 0, 0);
@@ -318,16 +353,41 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
 #pragma unroll
       for (int kk = 0; kk < kSteps; ++kk)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) q[nr][kk].w[j] = pack2_f16(ldexpf(x[kk][2 * j], -e), ldexpf(x[kk][2 * j + 1], -e));
+        for (int j = 0; j < 4; ++j) {
+          const float u = ldexpf(x[kk][2 * j], -e), w = ldexpf(x[kk][2 * j + 1], -e);
+          q[nr][kk].w[j] = pack2_f16(u, w);
+          if constexpr (kWindows) {
+            turned_q[kk][2 * j] = u;
+            turned_q[kk][2 * j + 1] = w;
+          }
+        }
     }
+    auto next_window = [&]() {  // the queries as seen from 2 kTreeTile positions further on
+#pragma unroll
+      for (int kk = 0; kk < kSteps / 2; ++kk)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float2 w = tail.back[8 * (4 * kk + g) + j];
+          float &lo = turned_q[kk][j], &hi = turned_q[kk + kSteps / 2][j];
+          const float y = lo * w.x + hi * w.y;
+          hi = hi * w.x - lo * w.y;
+          lo = y;
+        }
+#pragma unroll
+      for (int kk = 0; kk < kSteps; ++kk)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) q[0][kk].w[j] = pack2_f16(turned_q[kk][2 * j], turned_q[kk][2 * j + 1]);
+    };
+    if (kWindows && !win_kept) keep_window();
 
-    floatx4 o[kTiles][kDims];
+    floatx4 o[kTiles][kDims], ones[kTiles];  // ones: products of P with ones, i.e. sums of the weights (bf16 pages)
     float top[kTiles], ref[kTiles], sum[kTiles], least[kTiles];  // reference maximum, the same or 0, sum of weights, least score
 #pragma unroll
     for (int nr = 0; nr < kTiles; ++nr) {
       top[nr] = -INFINITY;
       ref[nr] = sum[nr] = 0.f;
       least[nr] = INFINITY;
+      ones[nr] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int dt = 0; dt < kDims; ++dt) o[nr][dt] = floatx4{0.f, 0.f, 0.f, 0.f};
     }
@@ -355,7 +415,7 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
 
     int mask_used = -1;  // what the products of the last staged tile need
     float ks_used = 0.f, vs_used = 0.f;
-    auto stage = [&](int t) {  // tile t into its buffer, and the loads of tile t + 1
+    auto stage = [&](auto odd, int t) {  // tile t (the second one of its window if odd) into its buffer, and the loads of tile t + 1
       unsigned char* buf = lds + (t & 1) * kTileBytes;
       const int first = t * kTreeTile, slots_left = r.kv_len - first;
       const bool has_nodes = first + kTreeTile > r.ctx;
@@ -368,68 +428,101 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
 #pragma unroll
       for (int i = 0; i < kHalves; ++i) {
         const int s = sl + i * kTurn, n = first + s;
-        int pos = n;
-        if (starts) pos = of_slot(start, t, s) + (s & (P - 1));
-        if (has_nodes) {
-          if (n >= r.ctx) pos = tail.node_pos[(n - r.ctx) & (MEPIC_TREE_MAX_NODES - 1)];
-          if (n >= r.kv_len) pos = pos_now + kTurn;
-        }
-        bool on = !(fresh && i == 0);
-        if (starts || has_nodes) on = on && __all(pos == pos_now + kTurn);
-        pos_now = pos;
-        if (on) {
+        Frag lo, hi;
+        if constexpr (kWindows) {
+          f16x2 (&c)[4] = win_c[decltype(odd)::value * kHalves + i], (&sn2)[4] = win_s[decltype(odd)::value * kHalves + i];
+          if (has_nodes) {  // slots of nodes stand anywhere
+            asm volatile("");
+            const int seen = first - decltype(odd)::value * kTreeTile;  // where the window begins
+            const int pos = n < r.ctx ? n - seen : (int)((uint32_t)tail.node_pos[(n - r.ctx) & (MEPIC_TREE_MAX_NODES - 1)] - (uint32_t)seen);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float y = sn[e] * turn_s[e];  // (in this order in place: no register is copied)
-            sn[e] *= turn_c[e];
-            sn[e] = __builtin_fmaf(cs[e], turn_s[e], sn[e]);
-            cs[e] = __builtin_fmaf(cs[e], turn_c[e], -y);
+            for (int j = 0; j < 4; ++j) {
+              const int i0 = freq_index(2 * j), i1 = freq_index(2 * j + 1);
+              const float f0 = turns_frac((float)pos, a.freq_hi[i0], a.freq_lo[i0]), f1 = turns_frac((float)pos, a.freq_hi[i1], a.freq_lo[i1]);
+              c[j] = __builtin_bit_cast(f16x2, pack2_f16(__builtin_amdgcn_cosf(f0), __builtin_amdgcn_cosf(f1)));
+              sn2[j] = __builtin_bit_cast(f16x2, pack2_f16(__builtin_amdgcn_sinf(f0), __builtin_amdgcn_sinf(f1)));
+            }
+            win_kept = false;
           }
-        } else {
+          uint32_t x[8];  // low dims, high dims
+          if constexpr (kFp8) {
+            const uint32_t w[4] = {d.k[i].lo.x, d.k[i].lo.y, d.k[i].hi.x, d.k[i].hi.y};
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const int j = freq_index(e);
-            const float f = turns_frac((float)pos, a.freq_hi[j], a.freq_lo[j]);
-            cs[e] = kKeyFactor * __builtin_amdgcn_cosf(f);
-            sn[e] = kKeyFactor * __builtin_amdgcn_sinf(f);
+            for (int j = 0; j < 8; ++j) x[j] = f16_of_e4m3(w[j >> 1], j & 1);
+          } else {
+            const uint32_t w[8] = {d.k[i].lo.x, d.k[i].lo.y, d.k[i].lo.z, d.k[i].lo.w, d.k[i].hi.x, d.k[i].hi.y, d.k[i].hi.z, d.k[i].hi.w};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = pack2_f16(__uint_as_float(w[j] << 16), __uint_as_float(w[j] & 0xffff0000u));
           }
-        }
-        float x[16];  // low dims, high dims
-        if constexpr (kFp8) {
-          const uint32_t w[4] = {d.k[i].lo.x, d.k[i].lo.y, d.k[i].hi.x, d.k[i].hi.y};
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const f32x2 p0 = __builtin_amdgcn_cvt_pk_f32_fp8(w[j], false), p1 = __builtin_amdgcn_cvt_pk_f32_fp8(w[j], true);
-            x[4 * j] = p0[0]; x[4 * j + 1] = p0[1]; x[4 * j + 2] = p1[0]; x[4 * j + 3] = p1[1];
+            const f16x2 u = __builtin_bit_cast(f16x2, x[j]), w = __builtin_bit_cast(f16x2, x[4 + j]);
+            lo.w[j] = __builtin_bit_cast(uint32_t, u * c[j] - w * sn2[j]);
+            hi.w[j] = __builtin_bit_cast(uint32_t, w * c[j] + u * sn2[j]);
           }
         } else {
-          const uint32_t w[8] = {d.k[i].lo.x, d.k[i].lo.y, d.k[i].lo.z, d.k[i].lo.w, d.k[i].hi.x, d.k[i].hi.y, d.k[i].hi.z, d.k[i].hi.w};
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            x[2 * j] = __uint_as_float(w[j] << 16);
-            x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+          int pos = n;
+          if (starts) pos = of_slot(start, t, s) + (s & (P - 1));
+          if (has_nodes) {
+            if (n >= r.ctx) pos = tail.node_pos[(n - r.ctx) & (MEPIC_TREE_MAX_NODES - 1)];
+            if (n >= r.kv_len) pos = pos_now + kTurn;
           }
-        }
-        if (inter) {  // pairs are neighbours: four of the low dims, four of the high ones
+          bool on = !(fresh && i == 0);
+          if (starts || has_nodes) on = on && __all(pos == pos_now + kTurn);
+          pos_now = pos;
+          if (on) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float y = x[2 * e] * cs[e] - x[2 * e + 1] * sn[e];
-            x[2 * e + 1] = x[2 * e + 1] * cs[e] + x[2 * e] * sn[e];
-            x[2 * e] = y;
+            for (int e = 0; e < 8; ++e) {
+              const float y = sn[e] * turn_s[e];  // (in this order in place: no register is copied)
+              sn[e] *= turn_c[e];
+              sn[e] = __builtin_fmaf(cs[e], turn_s[e], sn[e]);
+              cs[e] = __builtin_fmaf(cs[e], turn_c[e], -y);
+            }
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const int j = freq_index(e);
+              const float f = turns_frac((float)pos, a.freq_hi[j], a.freq_lo[j]);
+              cs[e] = kKeyFactor * __builtin_amdgcn_cosf(f);
+              sn[e] = kKeyFactor * __builtin_amdgcn_sinf(f);
+            }
           }
-        } else {
+          float x[16];  // low dims, high dims
+          if constexpr (kFp8) {
+            const uint32_t w[4] = {d.k[i].lo.x, d.k[i].lo.y, d.k[i].hi.x, d.k[i].hi.y};
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float y = x[e] * cs[e] - x[8 + e] * sn[e];
-            x[8 + e] = x[8 + e] * cs[e] + x[e] * sn[e];
-            x[e] = y;
+            for (int j = 0; j < 4; ++j) {
+              const f32x2 p0 = __builtin_amdgcn_cvt_pk_f32_fp8(w[j], false), p1 = __builtin_amdgcn_cvt_pk_f32_fp8(w[j], true);
+              x[4 * j] = p0[0]; x[4 * j + 1] = p0[1]; x[4 * j + 2] = p1[0]; x[4 * j + 3] = p1[1];
+            }
+          } else {
+            const uint32_t w[8] = {d.k[i].lo.x, d.k[i].lo.y, d.k[i].lo.z, d.k[i].lo.w, d.k[i].hi.x, d.k[i].hi.y, d.k[i].hi.z, d.k[i].hi.w};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              x[2 * j] = __uint_as_float(w[j] << 16);
+              x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+            }
           }
-        }
-        Frag lo, hi;
+          if (inter) {  // pairs are neighbours: four of the low dims, four of the high ones
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          lo.w[j] = pack2_f16(x[2 * j], x[2 * j + 1]);
-          hi.w[j] = pack2_f16(x[8 + 2 * j], x[9 + 2 * j]);
+            for (int e = 0; e < 8; ++e) {
+              const float y = x[2 * e] * cs[e] - x[2 * e + 1] * sn[e];
+              x[2 * e + 1] = x[2 * e + 1] * cs[e] + x[2 * e] * sn[e];
+              x[2 * e] = y;
+            }
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const float y = x[e] * cs[e] - x[8 + e] * sn[e];
+              x[8 + e] = x[8 + e] * cs[e] + x[e] * sn[e];
+              x[e] = y;
+            }
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            lo.w[j] = pack2_f16(x[2 * j], x[2 * j + 1]);
+            hi.w[j] = pack2_f16(x[8 + 2 * j], x[9 + 2 * j]);
+          }
         }
         bool live = n < r.kv_len;
         if (masks) {
@@ -577,6 +670,8 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
             ref[nr] = now_top == -INFINITY ? 0.f : now_top;
             sum[nr] *= f;
 #pragma unroll
+            for (int i = 0; i < 4; ++i) ones[nr][i] *= f;
+#pragma unroll
             for (int dt = 0; dt < kDims; ++dt)
 #pragma unroll
               for (int i = 0; i < 4; ++i) o[nr][dt][i] *= f;
@@ -586,19 +681,24 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             y[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(y[j], c, shift));
-            part += y[j];
+            if (kFp8) part += y[j];
           }
           if constexpr (kFp8) {
             sum[nr] = __builtin_fmaf(part, vi, sum[nr]);
 #pragma unroll
             for (int j = 0; j < 4; ++j) p[nr].w[j] = pack2_f16(y[2 * j] * vm, y[2 * j + 1] * vm);
           } else {
-            sum[nr] += part;
 #pragma unroll
             for (int j = 0; j < 4; ++j) p[nr].w[j] = pack2_bf16(y[2 * j], y[2 * j + 1]);
           }
         }
         __builtin_amdgcn_sched_barrier(0);
+        if constexpr (!kFp8) {
+          Frag one;
+          one.w[0] = one.w[1] = one.w[2] = one.w[3] = 0x3f803f80u;
+#pragma unroll
+          for (int nr = 0; nr < kTiles; ++nr) ones[nr] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(one.v, p[nr].v, ones[nr], 0, 0, 0);
+        }
 #pragma unroll
         for (int dt = 0; dt < kDims; ++dt) {
 #pragma unroll
@@ -614,20 +714,23 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
       }
     };
 
-    // Of a SIMD's two waves one stages a tile before the products of the one in front, the other after them: vector and matrix
-    // instructions of the two meet.
-    const bool early = wave < 4;
-    stage(t0);
+    constexpr std::integral_constant<int, 0> kEven;
+    constexpr std::integral_constant<int, kWindows ? 1 : 0> kOdd;
+    stage(kEven, t0);
     __syncthreads();
 #pragma unroll 1
-    for (int t = t0; t < t1; ++t) {
-      const int mask0 = mask_used;
-      const float ks0 = ks_used, vs0 = vs_used;
-      const bool more = t + 1 < t1;
-      if (early && more) stage(t + 1);
-      if (busy) products(t, mask0, ks0, vs0);
-      if (!early && more) stage(t + 1);
+    for (int t = t0;;) {
+      if (busy) products(t, mask_used, ks_used, vs_used);
+      if (t + 1 < t1) stage(kOdd, t + 1);
       __syncthreads();
+      if (++t == t1) break;
+      if constexpr (kWindows) {
+        if (busy) products(t, mask_used, ks_used, vs_used);
+        if (t + 1 < t1) stage(kEven, t + 1);
+        __syncthreads();
+        if (++t == t1) break;
+        if (busy) next_window();
+      }
     }
 
     // ---- the waves of a group of rows merged, rows written ----
@@ -635,7 +738,7 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
     if (busy) {
 #pragma unroll
       for (int nr = 0; nr < kTiles; ++nr) {
-        const float total_w = sum_over_kgroups(sum[nr]);
+        const float total_w = kFp8 ? sum_over_kgroups(sum[nr]) : ones[nr][0];
         const float low = -max_over_kgroups(-least[nr]);
         const int row = nr * 16 + n16;
         if (g == 0) {

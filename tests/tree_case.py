@@ -127,16 +127,20 @@ class TreeCase:
 
 
 def bound(case, want, kernel):
-    """How far a right result may be from `want`, element by element. Relative errors of the operands of a score: fp16 keys and queries
-    2^-11 each (matrix-core kernels on 16- and 8-bit pages); fp32 operands, sums of 128 products and phases of 1e-7 turns 1e-5 in all.
+    """How far a right result may be from `want`, element by element. `size` is scale * sum over pairs |q||k|, which bounds sum |q_i k_i| in any
+    rotation. fp32 operands, sums of 128 products and phases of 1e-7 turns: 1e-5 of it in all. Matrix-core kernels on 16- and 8-bit
+    pages: a key's element u c - w s has its cos and sin, its first product and its sum rounded to fp16, 2^-11 each of |u c| + |w s| <= |k| at
+    most, so 3 sqrt(2) 2^-11 |k| for the pair; a query's pair 2^-11 |q|; together 5.25 x 2^-11 of `size`.
     A score that is off by d puts e^(2d) on weight over sum of weights; probabilities are rounded by 2^-8 (bf16) or less, sums of
     weights and of the products of 32 slots by 2^-24 a step; the result once to its own type."""
     out, mean, size = want
     f32 = case.kv_dtype == "f32"
     fine = f32 or kernel == "tree_general"
-    d = size * (1e-5 if fine else 2.0 ** -10 + 1e-5)
+    d = size * (1e-5 if fine else 5.25 * 2.0 ** -11 + 1e-5)
     steps = (int(case.kv.max()) if fine else int(case.kv.max()) / 32 + 64) * 2.0 ** -24
-    rel = np.expm1(2 * d)[..., None] + (0 if fine else 2.0 ** -8) + steps + 2.0 ** -20
+    with np.errstate(over="ignore"):
+        weight = np.expm1(2 * d)[..., None]
+    rel = weight + (0 if fine else 2.0 ** -8) + steps + 2.0 ** -20
     return mean * rel + np.abs(out) * (2.0 ** -23 if f32 else 2.0 ** -8) + 1e-30
 
 
