@@ -116,11 +116,12 @@ TreePlan tree_mfma_plan(const TreeArgs& t, int max_kv) {
   const long row_bound = (long)t.max_q * a.G;
   p.rows = row_bound <= 32 ? 32 : row_bound <= 64 ? 64 : row_bound <= 128 ? 128 : 256;
   const int cus = device_compute_units();
-  p.groups = cus / a.Hkv > 1 ? cus / a.Hkv : 1;
-  const long tiles = (max_kv + kTreeTile - 1) / kTreeTile;
+  const int resident = p.rows == 256 ? cus : 2 * cus;  // workgroups of eight and of four waves
+  p.groups = resident / a.Hkv > 1 ? resident / a.Hkv : 1;
+  const long tiles = (max_kv + 63) / 64;
   if (((long)a.n_q * a.G / p.rows + a.B + 1) * (tiles + 1) > (1L << 30)) return TreePlan{};  // (the work is counted in 32 bits)
-  p.whole = tiles <= 4;
-  p.min_tiles = 2;
+  p.whole = tiles <= 8;
+  p.min_slots = 256;
   if (!p.whole)
     p.bytes = (size_t)p.groups * a.Hkv * 2 * p.rows * (a.D + 2) * sizeof(float) + (size_t)a.n_q * a.G * sizeof(int4);
   return p;
@@ -130,7 +131,7 @@ hipError_t launch_tree_mfma(const TreeArgs& t, const TreePlan& pl, void* workspa
   const AttnArgs& a = t.a;
   TreeMfmaArgs m{};
   m.t = t;
-  m.groups = pl.groups; m.min_tiles = pl.min_tiles; m.whole = pl.whole;
+  m.groups = pl.groups; m.min_slots = pl.min_slots; m.whole = pl.whole;
   const size_t parts = (size_t)pl.groups * a.Hkv * 2 * pl.rows;
   m.row_wgs = static_cast<int4*>(workspace);
   m.part_o = reinterpret_cast<float*>(m.row_wgs + (size_t)a.n_q * a.G);

@@ -5,27 +5,23 @@
 namespace mepic {
 namespace {
 
-template <int D, int kGroups, int kTiles, bool kPlain>
+template <int D, int kWaves, int kGroups, int kTiles, bool kPlain>
 hipError_t launch_one(const TreeMfmaArgs& m, hipStream_t s) {
   static std::atomic<uint64_t> asked{0};
-  const auto kernel = tree_tiles_kernel<true, D, kGroups, kTiles, kPlain>;
-  constexpr size_t bytes = tree_lds_bytes<D>();
+  const auto kernel = tree_tiles_kernel<true, D, kWaves, kGroups, kTiles, kPlain>;
+  constexpr size_t bytes = tree_lds_bytes<D, kWaves>();
   const hipError_t e = allow_lds(reinterpret_cast<const void*>(kernel), bytes, asked);
   if (e != hipSuccess) return e;
-  kernel<<<dim3((unsigned)m.groups * m.t.a.Hkv), dim3(kTreeThreads), bytes, s>>>(m);
+  kernel<<<dim3((unsigned)m.groups * m.t.a.Hkv), dim3(kWaves * 64), bytes, s>>>(m);
   return hipGetLastError();
 }
 
 template <int D, bool kPlain>
 hipError_t launch_rows(int rows, const TreeMfmaArgs& m, hipStream_t s) {
-  if (rows == 32) return launch_one<D, 2, 1, kPlain>(m, s);
-#ifdef V64
-  if (rows == 64) return launch_one<D, 2, 2, kPlain>(m, s);
-#else
-  if (rows == 64) return launch_one<D, 4, 1, kPlain>(m, s);
-#endif
-  if (rows == 128) return launch_one<D, 4, 2, kPlain>(m, s);
-  return launch_one<D, 8, 2, kPlain>(m, s);
+  if (rows == 32) return launch_one<D, 4, 2, 1, kPlain>(m, s);
+  if (rows == 64) return launch_one<D, 4, 4, 1, kPlain>(m, s);
+  if (rows == 128) return launch_one<D, 4, 4, 2, kPlain>(m, s);
+  return launch_one<D, 8, 8, 2, kPlain>(m, s);
 }
 
 }  // namespace

@@ -189,15 +189,14 @@ __device__ __forceinline__ int request_of(const int32_t* cu, int B, int t) {
 struct TreePlan {
   int rows;        // rows of a workgroup's tile: 32, 64, 128, 256
   int groups;      // workgroups per KV head
-  int min_tiles;   // least run of a workgroup, in tiles of kTreeTile slots
+  int min_slots;   // least run of a workgroup
   bool whole;      // a workgroup takes whole items (row tiles of a request): nothing to merge
   size_t bytes;    // workspace
 };
-constexpr int kTreeTile = 128;
 
 struct TreeMfmaArgs {
   TreeArgs t;
-  int32_t groups, min_tiles, whole;
+  int32_t groups, min_slots, whole;
   float* part_o;     // [groups * Hkv][2][rows][D]
   float* part_ml;    // [groups * Hkv][2][rows][2]
   int4* row_wgs;     // [n_q * G] first and last workgroup (of a KV head) that a row's item is cut for, row of the tile, request

@@ -28,23 +28,25 @@
 
 namespace mepic {
 
-constexpr int kTreeThreads = 512;
 constexpr int kReseed = 16;  // tiles after which cos and sin are found anew
 
+template <int kWaves>
 struct TreeLdsTail {  // behind the two tile buffers
   TreeArgs args;  // what the loop over tiles does not need is read from here: kernel arguments would fill the scalar registers
   uint32_t path[MEPIC_TREE_MAX_NODES][kTreeWords];
   int16_t parent[MEPIC_TREE_MAX_NODES];
   int node_pos[MEPIC_TREE_MAX_NODES];
   float2 back[kMaxHalfD];  // cos and sin of a window's turn
-  float ml[8][32][2];
-  int bad[256];
-  int scan[16];
+  float ml[kWaves][32][2];
+  int bad[kWaves * 32];
+  int scan[kWaves * 2];
   int found[2];
-  TreeRowLds<kTreeThreads> row;
+  TreeRowLds<kWaves * 64> row;
 };
 
-template <int D> constexpr size_t tree_lds_bytes() { return 2 * (size_t)kTreeTile * D * 2 * 2 + sizeof(TreeLdsTail); }
+// Two tiles of K and V operands and the tail: with four waves two workgroups of D 128 fit a compute unit.
+template <int D, int kWaves> constexpr size_t tree_lds_bytes() { return 2 * (size_t)(16 * kWaves) * D * 2 * 2 + sizeof(TreeLdsTail<kWaves>); }
+static_assert(2 * tree_lds_bytes<128, 4>() <= 160 * 1024);
 
 __device__ __forceinline__ uint32_t pack2_f16(float lo, float hi) {
   const f32x2 v = {lo, hi};
@@ -69,19 +71,24 @@ __device__ __forceinline__ uint32_t path_bits(const uint32_t* path, int n0, int 
   return s && w + 1 < kTreeWords ? lo | (path[w + 1] << (32 - s)) : lo;
 }
 
-template <bool kFp8, int D, int kGroups, int kTiles, bool kPlain>
-__global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeMfmaArgs m) {
-  constexpr int kRows = kGroups * kTiles * 16, kSlotGroups = 8 / kGroups, kSubs = 4 / kSlotGroups;
+template <bool kFp8, int D, int kWaves, int kGroups, int kTiles, bool kPlain>
+__global__ __launch_bounds__(kWaves * 64, 2) void tree_tiles_kernel(const TreeMfmaArgs m) {
+  constexpr int kThreads = kWaves * 64, kTile = 16 * kWaves;  // slots of a tile
+  constexpr int kRows = kGroups * kTiles * 16, kSlotGroups = kWaves / kGroups, kSubs = kTile / 32 / kSlotGroups;
+  static_assert(kSubs >= 1, "a wave has at least 32 slots of a tile");
   constexpr int kSteps = D / 32, kDims = D / 16;          // products per score, 16-dim tiles of O
   constexpr int E = kFp8 ? 1 : 2, X = 16 / E, DX = D / X;  // bytes per element, elements per granule
-  constexpr int kHalves = D / 64, kTurn = kTreeTile / kHalves;  // slots per thread of a tile, how far apart
-  constexpr int kKeyBytes = kTreeTile * D * 2, kTileBytes = 2 * kKeyBytes;
+  // a thread stages kHalves octets of dims: of D 128 eight waves have one octet of two slots each, four waves two octets of one slot
+  constexpr int kHalves = D / 64, kSlotStep = kWaves == 8 && D == 128 ? 64 : 0, kOctetStep = kWaves == 4 && D == 128 ? 4 : 0;
+  constexpr int kTurn = kSlotStep ? kSlotStep : kTile;  // positions from a thread's slot to its next
+  constexpr int kSets = kOctetStep ? kHalves : 1;       // octets whose cos and sin a thread has
+  constexpr int kKeyBytes = kTile * D * 2, kTileBytes = 2 * kKeyBytes;
   constexpr int kVGranules = 16 * D * E / 16 / 64;        // 16-byte pieces of V per lane and tile
   constexpr int kRing = kTiles == 1 && D == 128 ? 8 : 4;  // operands in flight: some 150 clocks a read, 16 a product
   constexpr bool kWindows = kPlain && kTiles == 1;  // keys turned from the start of a window of two tiles (see Staging)
   constexpr float kKeyFactor = kFp8 || kWindows ? 1.f : 16.f;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-  TreeLdsTail& tail = *reinterpret_cast<TreeLdsTail*>(lds + 2 * kTileBytes);
+  TreeLdsTail<kWaves>& tail = *reinterpret_cast<TreeLdsTail<kWaves>*>(lds + 2 * kTileBytes);
   const TreeArgs& ta = tail.args;
   const AttnArgs& a = ta.a;
   const AttnArgs& hot = m.t.a;
@@ -98,7 +105,7 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
     tail.args.a.freq_hi[tid] = m.t.a.freq_hi[tid];
     tail.args.a.freq_lo[tid] = m.t.a.freq_lo[tid];
     if (kWindows) {
-      const float f = turns_frac(2.f * kTreeTile, m.t.a.freq_hi[tid], m.t.a.freq_lo[tid]);
+      const float f = turns_frac(2.f * kTile, m.t.a.freq_hi[tid], m.t.a.freq_lo[tid]);
       tail.back[tid] = make_float2(__builtin_amdgcn_cosf(f), __builtin_amdgcn_sinf(f));
     }
   }
@@ -107,11 +114,11 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
   // ---- this workgroup's run: [begin, end) of the (item, tile) pairs of all requests ----
   auto cost_of = [&](int b, int& tiles, int& items) {
     const TreeRequest r = tree_request(a, b);
-    tiles = max((r.kv_len + kTreeTile - 1) / kTreeTile, 1);
+    tiles = max((r.kv_len + kTile - 1) / kTile, 1);
     items = (min(r.T, ta.max_q) * G + kRows - 1) / kRows;
     return m.whole ? items : items * tiles;
   };
-  // inclusive prefix sums of the costs of 512 requests; returns their total
+  // inclusive prefix sums of the costs of kThreads requests; returns their total
   auto scan_costs = [&](int b0, int& incl, int& cost) {
     int tiles, items;
     cost = b0 + tid < a.B ? cost_of(b0 + tid, tiles, items) : 0;
@@ -125,7 +132,7 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
     __syncthreads();
     int before = 0, total = 0;
 #pragma unroll
-    for (int w = 0; w < 8; ++w) {
+    for (int w = 0; w < kWaves; ++w) {
       const int x = tail.scan[w];
       if (w < wave) before += x;
       total += x;
@@ -135,17 +142,17 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
     return total;
   };
   int incl, cost, total = scan_costs(0, incl, cost);
-  for (int b0 = kTreeThreads; b0 < a.B; b0 += kTreeThreads) {
+  for (int b0 = kThreads; b0 < a.B; b0 += kThreads) {
     int i2, c2;
     total += scan_costs(b0, i2, c2);
   }
-  const int per = max((total + m.groups - 1) / m.groups, m.whole ? 1 : m.min_tiles);
+  const int per = max((total + m.groups - 1) / m.groups, m.whole ? 1 : m.min_slots / kTile);
   int at = wg * per;
   const int end = min(total, at + per);
   if (at >= end) return;
   int b = 0, before = 0;  // the request of `at`, and the cost of those in front of it
   {
-    int base = 0, sum = a.B > kTreeThreads ? scan_costs(0, incl, cost) : total;
+    int base = 0, sum = a.B > kThreads ? scan_costs(0, incl, cost) : total;
     for (int b0 = 0;; ) {
       if (cost > 0 && base + incl - cost <= at && at < base + incl) {
         tail.found[0] = b0 + tid;
@@ -153,7 +160,7 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
       }
       if (at < base + sum) break;
       base += sum;
-      b0 += kTreeThreads;
+      b0 += kThreads;
       sum = scan_costs(b0, incl, cost);
     }
     __syncthreads();
@@ -161,42 +168,50 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
     before = uni(tail.found[1]);
   }
 
-  // ---- what a thread stages: the eight pairs of octet pc (the wave's) of slots sl and, D 128, sl + 64; in LDS a slot lies at `place` ----
-  const int pc = D == 128 ? wave : wave & 3, place = D == 128 ? lane : (wave >> 2) * 64 + lane;
+  // ---- what a thread stages: the eight pairs of octet pc (the wave's) of slot sl, then those kOctetStep octets and kSlotStep slots on;
+  // in LDS a slot lies at `place` ----
+  const int pc = wave & (D / 16 - 1), place = (D == 64 && kWaves == 8 ? (wave >> 2) * 64 : 0) + lane;
   const int sl = (place & ~31) | ((place & 12) << 1) | ((place & 16) >> 2) | (place & 3);
-  float turn_c[8], turn_s[8];  // the turn by kTurn positions
+  float turn_c[kSets][8], turn_s[kSets][8];  // the turn by kTurn positions
   const bool inter = !kPlain && hot.interleaved;
-  auto freq_index = [&](int e) { return !inter ? 8 * pc + e : e < 4 ? 4 * pc + e : D / 4 + 4 * pc + e - 4; };
+  auto freq_index = [&](int i, int e) {
+    const int c = pc + i * kOctetStep;
+    return !inter ? 8 * c + e : e < 4 ? 4 * c + e : D / 4 + 4 * c + e - 4;
+  };
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const int i = freq_index(e);
-    const float f = turns_frac((float)kTurn, a.freq_hi[i], a.freq_lo[i]);
-    turn_c[e] = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(__builtin_amdgcn_cosf(f))));
-    turn_s[e] = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(__builtin_amdgcn_sinf(f))));
-  }
+  for (int i = 0; i < kSets; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float f = turns_frac((float)kTurn, a.freq_hi[freq_index(i, e)], a.freq_lo[freq_index(i, e)]);
+      turn_c[i][e] = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(__builtin_amdgcn_cosf(f))));
+      turn_s[i][e] = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(__builtin_amdgcn_sinf(f))));
+    }
   // kWindows: cos and sin of a thread's slots of a window, for two pairs a register
   f16x2 win_c[kWindows ? 2 * kHalves : 1][4], win_s[kWindows ? 2 * kHalves : 1][4];
   bool win_kept = false;
-  auto keep_window = [&]() {
-    float c[8], s[8];
+  auto keep_window = [&]() {  // [tile of the window * kHalves + half]
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float f = turns_frac((float)sl, a.freq_hi[freq_index(e)], a.freq_lo[freq_index(e)]);
-      c[e] = __builtin_amdgcn_cosf(f);
-      s[e] = __builtin_amdgcn_sinf(f);
-    }
-#pragma unroll
-    for (int h = 0; h < (kWindows ? 2 * kHalves : 1); ++h) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        win_c[h][j] = __builtin_bit_cast(f16x2, pack2_f16(c[2 * j], c[2 * j + 1]));
-        win_s[h][j] = __builtin_bit_cast(f16x2, pack2_f16(s[2 * j], s[2 * j + 1]));
-      }
+    for (int i = 0; i < kSets; ++i) {
+      float c[8], s[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float y = c[e] * turn_c[e] - s[e] * turn_s[e];
-        s[e] = s[e] * turn_c[e] + c[e] * turn_s[e];
-        c[e] = y;
+        const float f = turns_frac((float)sl, a.freq_hi[freq_index(i, e)], a.freq_lo[freq_index(i, e)]);
+        c[e] = __builtin_amdgcn_cosf(f);
+        s[e] = __builtin_amdgcn_sinf(f);
+      }
+#pragma unroll
+      for (int h = i; h < (kWindows ? 2 * kHalves : 1); h += kSets) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          win_c[h][j] = __builtin_bit_cast(f16x2, pack2_f16(c[2 * j], c[2 * j + 1]));
+          win_s[h][j] = __builtin_bit_cast(f16x2, pack2_f16(s[2 * j], s[2 * j + 1]));
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float y = c[e] * turn_c[i][e] - s[e] * turn_s[i][e];
+          s[e] = s[e] * turn_c[i][e] + c[e] * turn_s[i][e];
+          c[e] = y;
+        }
       }
     }
     win_kept = true;
@@ -213,7 +228,7 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
     const int octet = ((v_page << logP) >> 3) + v_part * (X / 8) + h;
     v_dst[h] = kKeyBytes + (octet * D + (v_dim ^ twist_of(octet))) * 16;
   }
-  const int k_src = (g * kTreeTile + n16) * 16, v_src = kKeyBytes + (g * D + (n16 ^ twist_of(g))) * 16;  // a lane's first operands
+  const int k_src = (g * kTile + n16) * 16, v_src = kKeyBytes + (g * D + (n16 ^ twist_of(g))) * 16;  // a lane's first operands
   const size_t page_bytes = (size_t)hot.Hkv * D * P * E, head_bytes = (size_t)hk * D * P * E;
   const unsigned char* kp = static_cast<const unsigned char*>(hot.k_pages) + head_bytes;
   const unsigned char* vp = static_cast<const unsigned char*>(hot.v_pages) + head_bytes;
@@ -238,12 +253,12 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
     // rows that other workgroups share: which ones (head 0 says so for all)
     if (!m.whole && t0 == 0 && hk == 0) {
       const int last = (before + rt * tiles + tiles - 1) / per;
-      for (int i = tid; i < min(n_rows, kRows); i += kTreeThreads) {
+      for (int i = tid; i < min(n_rows, kRows); i += kThreads) {
         m.row_wgs[(size_t)r.q0 * G + rt * kRows + i] = make_int4(wg, last, i, b);
       }
     }
     // paths, where the run has nodes among its slots
-    const bool nodes_here = t1 * kTreeTile > r.ctx;
+    const bool nodes_here = t1 * kTile > r.ctx;
     if (nodes_here) {
       const int T = min(r.T, MEPIC_TREE_MAX_NODES);
       if (tid < T) {
@@ -270,25 +285,27 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
 
     // ---- loads of a tile. Block tables, masks and positions come in windows of 64 blocks, a block a lane, two tiles ahead ----
     auto window = [&](const int32_t* rows, int t) {
-      return rows[bt_row + min((((t * kTreeTile) >> logP) & ~63) + lane, hot.max_blocks - 1)];
+      return rows[bt_row + min((((t * kTile) >> logP) & ~63) + lane, hot.max_blocks - 1)];
     };
-    auto in_window = [&](int t) { return ((t * kTreeTile) >> logP) & 63; };  // the tile's first block in its window
+    auto in_window = [&](int t) { return ((t * kTile) >> logP) & 63; };  // the tile's first block in its window
     auto of_slot = [&](int w, int t, int s) { return __builtin_amdgcn_ds_bpermute(4 * (in_window(t) + (s >> logP)), w); };
     auto of_block = [&](int w, int t, int blk) { return __builtin_amdgcn_readlane(w, in_window(t) + blk); };
     auto in_pool = [&](int page) { return (size_t)max(min(page, hot.num_pages - 1), 0); };
+    constexpr int kPages = kSlotStep ? kHalves : 1;
     struct Keys { typename std::conditional<kFp8, uint2, uint4>::type lo, hi; };  // eight elements each
     struct Data { Keys k[kHalves]; uint4 v[kVGranules]; };
-    auto load_k = [&](Data& d, const int (&page)[kHalves]) {
+    auto load_k = [&](Data& d, const int (&page)[kPages]) {
       const int s = sl & (P - 1);
 #pragma unroll
       for (int i = 0; i < kHalves; ++i) {
-        const unsigned char* pk = kp + in_pool(page[i]) * page_bytes;
+        const unsigned char* pk = kp + in_pool(page[kSlotStep ? i : 0]) * page_bytes;
+        const int c = pc + i * kOctetStep;
         if constexpr (kFp8) {  // half a granule
-          pk += ((pc >> 1) * P + s) * 16 + (pc & 1) * 8;
+          pk += ((c >> 1) * P + s) * 16 + (c & 1) * 8;
           d.k[i].lo = *reinterpret_cast<const uint2*>(pk);
           d.k[i].hi = *reinterpret_cast<const uint2*>(pk + DX / 2 * P * 16);
         } else {
-          pk += (pc * P + s) * 16;
+          pk += (c * P + s) * 16;
           d.k[i].lo = *reinterpret_cast<const uint4*>(pk);
           d.k[i].hi = *reinterpret_cast<const uint4*>(pk + DX / 2 * P * 16);
         }
@@ -301,7 +318,7 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
     };
 
     // ---- queries of the wave's rows ----
-    const int base = kWindows ? t0 * kTreeTile : 0;  // positions are counted from here
+    const int base = kWindows ? t0 * kTile : 0;  // positions are counted from here
     Frag q[kTiles][kSteps];
     float turned_q[kWindows ? kSteps : 1][8];
     float row_scale[kTiles];
@@ -362,7 +379,7 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
           }
         }
     }
-    auto next_window = [&]() {  // the queries as seen from 2 kTreeTile positions further on
+    auto next_window = [&]() {  // the queries as seen from 2 kTile positions further on
 #pragma unroll
       for (int kk = 0; kk < kSteps / 2; ++kk)
 #pragma unroll
@@ -393,7 +410,7 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
     }
     const bool busy = (rg * kTiles) * 16 < n_rows;  // does the wave have rows?
 
-    float cs[8], sn[8];
+    float cs[kSets][8], sn[kSets][8];
     int pos_now = 0;
     Data d;
     const int32_t* masks = kPlain || !hot.block_valid_mask ? nullptr : reinterpret_cast<const int32_t*>(hot.block_valid_mask);
@@ -401,9 +418,9 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
     int mask = masks ? window(masks, t0) : -1, start = starts ? window(starts, t0) : 0;  // of tile t, then of the next one
     const int second = min(t0 + 1, t1 - 1);
     int pages = window(hot.block_tables, t0), mask1 = masks ? window(masks, second) : -1, start1 = starts ? window(starts, second) : 0;
-    int k_page[kHalves];
+    int k_page[kPages];
 #pragma unroll
-    for (int i = 0; i < kHalves; ++i) k_page[i] = of_slot(pages, t0, sl + i * kTurn);
+    for (int i = 0; i < kPages; ++i) k_page[i] = of_slot(pages, t0, sl + i * kSlotStep);
     load_k(d, k_page);
     load_v(d, pages, t0);
     float k_scale = 0.f, v_scale = 0.f;
@@ -417,27 +434,28 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
     float ks_used = 0.f, vs_used = 0.f;
     auto stage = [&](auto odd, int t) {  // tile t (the second one of its window if odd) into its buffer, and the loads of tile t + 1
       unsigned char* buf = lds + (t & 1) * kTileBytes;
-      const int first = t * kTreeTile, slots_left = r.kv_len - first;
-      const bool has_nodes = first + kTreeTile > r.ctx;
+      const int first = t * kTile, slots_left = r.kv_len - first;
+      const bool has_nodes = first + kTile > r.ctx;
       const bool fresh = ((t - t0) & (kReseed - 1)) == 0;
+      bool on = false;
       // (loads always, the last tile's are its own again: a wait for some of them has to hold on every path. The exchange of page ids comes
       // before the writes to LDS: behind them it waits for them.)
       const int t2 = min(t + 1, t1 - 1), t3 = min(t + 2, t1 - 1);
 #pragma unroll
-      for (int i = 0; i < kHalves; ++i) k_page[i] = of_slot(pages, t2, sl + i * kTurn);
+      for (int i = 0; i < kPages; ++i) k_page[i] = of_slot(pages, t2, sl + i * kSlotStep);
 #pragma unroll
       for (int i = 0; i < kHalves; ++i) {
-        const int s = sl + i * kTurn, n = first + s;
+        const int s = sl + i * kSlotStep, n = first + s, set = kOctetStep ? i : 0;
         Frag lo, hi;
         if constexpr (kWindows) {
           f16x2 (&c)[4] = win_c[decltype(odd)::value * kHalves + i], (&sn2)[4] = win_s[decltype(odd)::value * kHalves + i];
           if (has_nodes) {  // slots of nodes stand anywhere
             asm volatile("");
-            const int seen = first - decltype(odd)::value * kTreeTile;  // where the window begins
+            const int seen = first - decltype(odd)::value * kTile;  // where the window begins
             const int pos = n < r.ctx ? n - seen : (int)((uint32_t)tail.node_pos[(n - r.ctx) & (MEPIC_TREE_MAX_NODES - 1)] - (uint32_t)seen);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              const int i0 = freq_index(2 * j), i1 = freq_index(2 * j + 1);
+              const int i0 = freq_index(set, 2 * j), i1 = freq_index(set, 2 * j + 1);
               const float f0 = turns_frac((float)pos, a.freq_hi[i0], a.freq_lo[i0]), f1 = turns_frac((float)pos, a.freq_hi[i1], a.freq_lo[i1]);
               c[j] = __builtin_bit_cast(f16x2, pack2_f16(__builtin_amdgcn_cosf(f0), __builtin_amdgcn_cosf(f1)));
               sn2[j] = __builtin_bit_cast(f16x2, pack2_f16(__builtin_amdgcn_sinf(f0), __builtin_amdgcn_sinf(f1)));
@@ -461,30 +479,33 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
             hi.w[j] = __builtin_bit_cast(uint32_t, w * c[j] + u * sn2[j]);
           }
         } else {
-          int pos = n;
-          if (starts) pos = of_slot(start, t, s) + (s & (P - 1));
-          if (has_nodes) {
-            if (n >= r.ctx) pos = tail.node_pos[(n - r.ctx) & (MEPIC_TREE_MAX_NODES - 1)];
-            if (n >= r.kv_len) pos = pos_now + kTurn;
+          if (!kOctetStep || i == 0) {
+            int pos = n;
+            if (starts) pos = of_slot(start, t, s) + (s & (P - 1));
+            if (has_nodes) {
+              if (n >= r.ctx) pos = tail.node_pos[(n - r.ctx) & (MEPIC_TREE_MAX_NODES - 1)];
+              if (n >= r.kv_len) pos = pos_now + kTurn;
+            }
+            on = !(fresh && i == 0);
+            if (starts || has_nodes) on = on && __all(pos == pos_now + kTurn);
+            pos_now = pos;
           }
-          bool on = !(fresh && i == 0);
-          if (starts || has_nodes) on = on && __all(pos == pos_now + kTurn);
-          pos_now = pos;
+          float (&c)[8] = cs[set], (&s2)[8] = sn[set];
           if (on) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-              const float y = sn[e] * turn_s[e];  // (in this order in place: no register is copied)
-              sn[e] *= turn_c[e];
-              sn[e] = __builtin_fmaf(cs[e], turn_s[e], sn[e]);
-              cs[e] = __builtin_fmaf(cs[e], turn_c[e], -y);
+              const float y = s2[e] * turn_s[set][e];  // (in this order in place: no register is copied)
+              s2[e] *= turn_c[set][e];
+              s2[e] = __builtin_fmaf(c[e], turn_s[set][e], s2[e]);
+              c[e] = __builtin_fmaf(c[e], turn_c[set][e], -y);
             }
           } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-              const int j = freq_index(e);
-              const float f = turns_frac((float)pos, a.freq_hi[j], a.freq_lo[j]);
-              cs[e] = kKeyFactor * __builtin_amdgcn_cosf(f);
-              sn[e] = kKeyFactor * __builtin_amdgcn_sinf(f);
+              const int j = freq_index(set, e);
+              const float f = turns_frac((float)pos_now, a.freq_hi[j], a.freq_lo[j]);
+              c[e] = kKeyFactor * __builtin_amdgcn_cosf(f);
+              s2[e] = kKeyFactor * __builtin_amdgcn_sinf(f);
             }
           }
           float x[16];  // low dims, high dims
@@ -506,15 +527,15 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
           if (inter) {  // pairs are neighbours: four of the low dims, four of the high ones
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-              const float y = x[2 * e] * cs[e] - x[2 * e + 1] * sn[e];
-              x[2 * e + 1] = x[2 * e + 1] * cs[e] + x[2 * e] * sn[e];
+              const float y = x[2 * e] * c[e] - x[2 * e + 1] * s2[e];
+              x[2 * e + 1] = x[2 * e + 1] * c[e] + x[2 * e] * s2[e];
               x[2 * e] = y;
             }
           } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-              const float y = x[e] * cs[e] - x[8 + e] * sn[e];
-              x[8 + e] = x[8 + e] * cs[e] + x[e] * sn[e];
+              const float y = x[e] * c[e] - x[8 + e] * s2[e];
+              x[8 + e] = x[8 + e] * c[e] + x[e] * s2[e];
               x[e] = y;
             }
           }
@@ -529,7 +550,7 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
           const int valid = of_slot(mask, t, s);  // (every lane takes part in the exchange)
           live = live && ((valid >> (s & (P - 1))) & 1);
         }
-        if (masks ? !__all(live) : slots_left < kTreeTile) {  // slots that take no part may hold anything
+        if (masks ? !__all(live) : slots_left < kTile) {  // slots that take no part may hold anything
           asm volatile("");  // (a branch, not eight selects in every tile)
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
@@ -537,9 +558,9 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
             hi.w[j] = live ? hi.w[j] : 0u;
           }
         }
-        unsigned char* dst = buf + (pc * kTreeTile + place + i * kTurn) * 16;
+        unsigned char* dst = buf + ((pc + i * kOctetStep) * kTile + place + i * kSlotStep) * 16;
         *reinterpret_cast<uint4*>(dst) = lo.u;
-        *reinterpret_cast<uint4*>(dst + D / 16 * kTreeTile * 16) = hi.u;
+        *reinterpret_cast<uint4*>(dst + D / 16 * kTile * 16) = hi.u;
         __builtin_amdgcn_sched_barrier(0);  // (one slot's widened keys in registers at a time)
       }
       load_k(d, k_page);
@@ -588,7 +609,7 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
     };
     auto products = [&](int t, int mask0, float ks0, float vs0) {
       const unsigned char* buf = lds + (t & 1) * kTileBytes;
-      const int first = t * kTreeTile, slots_left = r.kv_len - first;
+      const int first = t * kTile, slots_left = r.kv_len - first;
 #pragma unroll 1
       for (int sub = 0; sub < kSubs; ++sub) {
         const int grp = sg * kSubs + sub, n0 = first + 32 * grp;
@@ -598,7 +619,7 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
         // Operands come through a ring of kRing registers sets, each read right behind the product that frees its place; the order is
         // pinned (left to itself the compiler waits for each read before it requests the next).
         Frag k[kRing];
-        auto k_at = [&](int i) { return *reinterpret_cast<const uint4*>(buf + k_src + grp * 512 + (4 * (i >> 1) * kTreeTile + 16 * (i & 1)) * 16); };
+        auto k_at = [&](int i) { return *reinterpret_cast<const uint4*>(buf + k_src + grp * 512 + (4 * (i >> 1) * kTile + 16 * (i & 1)) * 16); };
 #pragma unroll
         for (int i = 0; i < kRing; ++i) k[i].u = k_at(i);
         __builtin_amdgcn_sched_barrier(0);
@@ -750,12 +771,12 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
         for (int dt = 0; dt < kDims; ++dt) *reinterpret_cast<floatx4*>(dst + 4 * ((4 * dt + g) ^ n16)) = o[nr][dt];
       }
     }
-    for (int i = tid; i < kRows; i += kTreeThreads) tail.bad[i] = 0;
+    for (int i = tid; i < kRows; i += kThreads) tail.bad[i] = 0;
     __syncthreads();
     const bool direct = t0 == 0 && t1 == tiles;
     constexpr int kQuads = D / 4;
     const size_t part = ((size_t)blockIdx.x * 2 + (t0 == 0 ? 1 : 0)) * kRows;
-    for (int u = tid; u < rows_here * kQuads; u += kTreeThreads) {
+    for (int u = tid; u < rows_here * kQuads; u += kThreads) {
       const int row = u / kQuads, quad = u % kQuads, in = row % (16 * kTiles), w0 = row / (16 * kTiles);
       float mx = -INFINITY;
 #pragma unroll
@@ -791,7 +812,7 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_tiles_kernel(const TreeM
       for (int row = 0; row < rows_here; ++row) {
         if (!tail.bad[row]) continue;
         const int all = rt * kRows + row, node = all / G, head = all - node * G;
-        tree_row<kFp8 ? MEPIC_F8E4M3 : MEPIC_BF16, kTreeThreads>(ta, tail.row, r, b, node, hk * G + head);
+        tree_row<kFp8 ? MEPIC_F8E4M3 : MEPIC_BF16, kThreads>(ta, tail.row, r, b, node, hk * G + head);
       }
     }
     at += m.whole ? 1 : t1 - t0;
