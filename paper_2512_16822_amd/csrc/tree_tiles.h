@@ -221,7 +221,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void tree_tiles_kernel(const TreeMf
   // slots, dim) lies at octet * D + (dim ^ twist): lanes that write together, of one dim and several octets, hit different banks
   const int v_per = P / X, v_part = (v_first + lane) & (v_per - 1), v_dim = (v_first + lane) >> (v_per == 1 ? 0 : v_per == 2 ? 1 : 2);
   const int v_stride = 64 / v_per * 16;  // (the dims of one lane are multiples of 16 apart: the twist is the same)
-  auto twist_of = [&](int octet) { return P == 16 ? (octet & 1) << 3 : (octet & 3) << 2; };
+  // (a read of 16 bytes a lane serves lanes 0-3, 12-15, 20-23, 24-27 together, then 4-11, 16-19, 28-31, and so on: octets 2i and 2i + 1 must keep
+  // dims 0-3 and 12-15 apart from 4-11, which 12 does; a write serves 16 consecutive lanes, two or four octets)
+  auto twist_of = [&](int octet) { return (octet & 1 ? 12 : 0) ^ (octet & 2 ? 4 : 0); };
   int v_dst[X / 8];
 #pragma unroll
   for (int h = 0; h < X / 8; ++h) {
