@@ -313,8 +313,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void tree_tiles_kernel(const TreeMf
         }
       }
     };
-    auto load_v = [&](Data& d, int pages, int t) {
-      const unsigned char* pv = vp + in_pool(of_block(pages, t, v_page)) * page_bytes + v_first * 16;
+    auto load_v = [&](Data& d, int page) {
+      const unsigned char* pv = vp + in_pool(page) * page_bytes + v_first * 16;
 #pragma unroll
       for (int i = 0; i < kVGranules; ++i) d.v[i] = *reinterpret_cast<const uint4*>(pv + (64 * i + lane) * 16);
     };
@@ -420,17 +420,22 @@ __global__ __launch_bounds__(kWaves * 64, 2) void tree_tiles_kernel(const TreeMf
     int mask = masks ? window(masks, t0) : -1, start = starts ? window(starts, t0) : 0;  // of tile t, then of the next one
     const int second = min(t0 + 1, t1 - 1);
     int pages = window(hot.block_tables, t0), mask1 = masks ? window(masks, second) : -1, start1 = starts ? window(starts, second) : 0;
-    int k_page[kPages];
-#pragma unroll
-    for (int i = 0; i < kPages; ++i) k_page[i] = of_slot(pages, t0, sl + i * kSlotStep);
-    load_k(d, k_page);
-    load_v(d, pages, t0);
+    int k_page[kPages], v_from;
     float k_scale = 0.f, v_scale = 0.f;
-    if constexpr (kFp8) {
-      k_scale = hot.k_scales[in_pool(pages)];
-      v_scale = hot.v_scales[in_pool(pages)];
-    }
-    pages = window(hot.block_tables, second);
+    // page ids of tile t for its loads, and its scales; then on to the window of tile `after`
+    auto take_pages = [&](int t, int after) {
+#pragma unroll
+      for (int i = 0; i < kPages; ++i) k_page[i] = of_slot(pages, t, sl + i * kSlotStep);
+      v_from = of_block(pages, t, v_page);
+      if constexpr (kFp8) {
+        k_scale = hot.k_scales[in_pool(pages)];
+        v_scale = hot.v_scales[in_pool(pages)];
+      }
+      pages = window(hot.block_tables, after);
+    };
+    take_pages(t0, second);
+    load_k(d, k_page);
+    load_v(d, v_from);
 
     int mask_used = -1;  // what the products of the last staged tile need
     float ks_used = 0.f, vs_used = 0.f;
@@ -440,11 +445,19 @@ __global__ __launch_bounds__(kWaves * 64, 2) void tree_tiles_kernel(const TreeMf
       const bool has_nodes = first + kTile > r.ctx;
       const bool fresh = ((t - t0) & (kReseed - 1)) == 0;
       bool on = false;
-      // (loads always, the last tile's are its own again: a wait for some of them has to hold on every path. The exchange of page ids comes
-      // before the writes to LDS: behind them it waits for them.)
+      // (loads always, the last tile's are its own again: a wait for some of them has to hold on every path. Ids, masks and scales come first:
+      // the next stage needs them first, and loads return in order. Their exchange behind the writes to LDS would wait for those.)
       const int t2 = min(t + 1, t1 - 1), t3 = min(t + 2, t1 - 1);
-#pragma unroll
-      for (int i = 0; i < kPages; ++i) k_page[i] = of_slot(pages, t2, sl + i * kSlotStep);
+      mask_used = mask;
+      const int start_used = start;
+      ks_used = k_scale;
+      vs_used = v_scale;
+      mask = mask1;
+      start = start1;
+      take_pages(t2, t3);
+      if (masks) mask1 = window(masks, t3);
+      if (starts) start1 = window(starts, t3);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int i = 0; i < kHalves; ++i) {
         const int s = sl + i * kSlotStep, n = first + s, set = kOctetStep ? i : 0;
@@ -483,7 +496,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void tree_tiles_kernel(const TreeMf
         } else {
           if (!kOctetStep || i == 0) {
             int pos = n;
-            if (starts) pos = of_slot(start, t, s) + (s & (P - 1));
+            if (starts) pos = of_slot(start_used, t, s) + (s & (P - 1));
             if (has_nodes) {
               if (n >= r.ctx) pos = tail.node_pos[(n - r.ctx) & (MEPIC_TREE_MAX_NODES - 1)];
               if (n >= r.kv_len) pos = pos_now + kTurn;
@@ -549,7 +562,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void tree_tiles_kernel(const TreeMf
         }
         bool live = n < r.kv_len;
         if (masks) {
-          const int valid = of_slot(mask, t, s);  // (every lane takes part in the exchange)
+          const int valid = of_slot(mask_used, t, s);  // (every lane takes part in the exchange)
           live = live && ((valid >> (s & (P - 1))) & 1);
         }
         if (masks ? !__all(live) : slots_left < kTile) {  // slots that take no part may hold anything
@@ -568,7 +581,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void tree_tiles_kernel(const TreeMf
       load_k(d, k_page);
       const int v_slot = v_page << logP;
       uint32_t v_bits = low_bits(slots_left - v_slot);  // of the page's slots those that take part
-      if (masks) v_bits &= (uint32_t)of_block(mask, t, v_page);
+      if (masks) v_bits &= (uint32_t)of_block(mask_used, t, v_page);
       const bool v_whole = (v_bits | ~low_bits(P)) == ~0u;
 #pragma unroll
       for (int i = 0; i < kVGranules; ++i) {
@@ -595,19 +608,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void tree_tiles_kernel(const TreeMf
           *reinterpret_cast<uint4*>(buf + v_dst[h] + i * v_stride) = f[h].u;
         }
       }
-      mask_used = mask;
-      ks_used = k_scale;
-      vs_used = v_scale;
-      load_v(d, pages, t2);
-      if constexpr (kFp8) {
-        k_scale = hot.k_scales[in_pool(pages)];
-        v_scale = hot.v_scales[in_pool(pages)];
-      }
-      mask = mask1;
-      start = start1;
-      pages = window(hot.block_tables, t3);
-      if (masks) mask1 = window(masks, t3);
-      if (starts) start1 = window(starts, t3);
+      load_v(d, v_from);
     };
     auto products = [&](int t, int mask0, float ks0, float vs0) {
       const unsigned char* buf = lds + (t & 1) * kTileBytes;
