@@ -740,20 +740,21 @@ __global__ __launch_bounds__(kWaves * 64, 2) void tree_tiles_kernel(const TreeMf
 
     constexpr std::integral_constant<int, 0> kEven;
     constexpr std::integral_constant<int, kWindows ? 1 : 0> kOdd;
-    stage(kEven, t0);
-    __syncthreads();
+    // (the loop is entered where the first tile is staged: one copy of the code less, which a short run would fetch for nothing)
 #pragma unroll 1
-    for (int t = t0;;) {
-      if (busy) products(t, mask_used, ks_used, vs_used);
-      if (t + 1 < t1) stage(kOdd, t + 1);
+    for (int t = t0 - 1;;) {
+      if (busy && t >= t0) products(t, mask_used, ks_used, vs_used);
+      if (t + 1 < t1) stage(kEven, t + 1);
       __syncthreads();
       if (++t == t1) break;
       if constexpr (kWindows) {
-        if (busy) products(t, mask_used, ks_used, vs_used);
-        if (t + 1 < t1) stage(kEven, t + 1);
+        if (busy) {
+          if (t > t0) next_window();
+          products(t, mask_used, ks_used, vs_used);
+        }
+        if (t + 1 < t1) stage(kOdd, t + 1);
         __syncthreads();
         if (++t == t1) break;
-        if (busy) next_window();
       }
     }
 
