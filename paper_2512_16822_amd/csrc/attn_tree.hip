@@ -113,10 +113,13 @@ TreePlan tree_mfma_plan(const TreeArgs& t, int max_kv) {
   const AttnArgs& a = t.a;
   TreePlan p{};
   if (a.max_blocks == 0 || a.num_pages == 0 || a.B == 0) return p;  // (no page to read)
-  const long row_bound = (long)t.max_q * a.G;
-  p.rows = row_bound <= 32 ? 32 : row_bound <= 64 ? 64 : row_bound <= 128 ? 128 : 256;
+  const long most = (long)t.max_q * a.G, mean = (long)a.n_q * a.G / a.B;  // rows of a request, at most and on average
+  if (most <= 32) p.rows = 32;
+  else if (most <= 64 || mean <= 64) p.rows = 64;
+  else if (a.kv_dtype == MEPIC_F8E4M3) p.rows = most <= 128 || mean <= 128 ? 128 : 256;
+  else p.rows = most <= 128 || mean <= 96 ? 64 : 256;
   const int cus = device_compute_units();
-  const int resident = p.rows == 256 ? cus : 2 * cus;  // workgroups of eight and of four waves
+  const int resident = p.rows == 32 || p.rows == 256 ? cus : 2 * cus;  // workgroups of eight and of four waves
   p.groups = resident / a.Hkv > 1 ? resident / a.Hkv : 1;
   const long tiles = (max_kv + 63) / 64;
   if (((long)a.n_q * a.G / p.rows + a.B + 1) * (tiles + 1) > (1L << 30)) return TreePlan{};  // (the work is counted in 32 bits)

@@ -18,7 +18,7 @@ hipError_t launch_one(const TreeMfmaArgs& m, hipStream_t s) {
 
 template <int D, bool kPlain>
 hipError_t launch_rows(int rows, const TreeMfmaArgs& m, hipStream_t s) {
-  if (rows == 32) return launch_one<D, 4, 2, 1, kPlain>(m, s);
+  if (rows == 32) return launch_one<D, 8, 2, 1, kPlain>(m, s);
   if (rows == 64) return launch_one<D, 4, 4, 1, kPlain>(m, s);
   if (rows == 128) return launch_one<D, 4, 4, 2, kPlain>(m, s);
   return launch_one<D, 8, 8, 2, kPlain>(m, s);

@@ -33,12 +33,13 @@ constexpr int kReseed = 16;  // tiles after which cos and sin are found anew
 template <int kWaves>
 struct TreeLdsTail {  // behind the two tile buffers
   TreeArgs args;  // what the loop over tiles does not need is read from here: kernel arguments would fill the scalar registers
+  float *part_o, *part_ml;
   uint32_t path[MEPIC_TREE_MAX_NODES][kTreeWords];
   int16_t parent[MEPIC_TREE_MAX_NODES];
   int node_pos[MEPIC_TREE_MAX_NODES];
   float2 back[kMaxHalfD];  // cos and sin of a window's turn
-  float ml[kWaves][32][2];
-  int bad[kWaves * 32];
+  float ml[kWaves][32][2];  // maxima and sums, where several waves share a row's slots
+  uint32_t bad[kWaves];  // a bit a row: to be computed again
   int scan[kWaves * 2];
   int found[2];
   TreeRowLds<kWaves * 64> row;
@@ -85,7 +86,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void tree_tiles_kernel(const TreeMf
   constexpr int kKeyBytes = kTile * D * 2, kTileBytes = 2 * kKeyBytes;
   constexpr int kVGranules = 16 * D * E / 16 / 64;        // 16-byte pieces of V per lane and tile
   constexpr int kRing = kTiles == 1 && D == 128 ? 8 : 4;  // operands in flight: some 150 clocks a read, 16 a product
-  constexpr bool kWindows = kPlain && kTiles == 1;  // keys turned from the start of a window of two tiles (see Staging)
+  constexpr bool kWindows = kPlain && kTiles == 1 && kSlotGroups == 1;  // keys turned from the start of a window of two tiles (see Staging)
   constexpr float kKeyFactor = kFp8 || kWindows ? 1.f : 16.f;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   TreeLdsTail<kWaves>& tail = *reinterpret_cast<TreeLdsTail<kWaves>*>(lds + 2 * kTileBytes);
@@ -100,7 +101,10 @@ __global__ __launch_bounds__(kWaves * 64, 2) void tree_tiles_kernel(const TreeMf
     __builtin_memcpy(&tail.args.a, &m.t.a, offsetof(AttnArgs, freq_hi));
     tail.args.parents = m.t.parents;
     tail.args.max_q = m.t.max_q;
+    tail.part_o = m.part_o;
+    tail.part_ml = m.part_ml;
   }
+  if (tid < kWaves) tail.bad[tid] = 0;
   if (tid < D / 2) {
     tail.args.a.freq_hi[tid] = m.t.a.freq_hi[tid];
     tail.args.a.freq_lo[tid] = m.t.a.freq_lo[tid];
@@ -314,9 +318,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void tree_tiles_kernel(const TreeMf
       }
     };
     auto load_v = [&](Data& d, int page) {
-      const unsigned char* pv = vp + in_pool(page) * page_bytes + v_first * 16;
+      const unsigned char* pv = vp + in_pool(page) * page_bytes;
 #pragma unroll
-      for (int i = 0; i < kVGranules; ++i) d.v[i] = *reinterpret_cast<const uint4*>(pv + (64 * i + lane) * 16);
+      for (int i = 0; i < kVGranules; ++i) d.v[i] = *reinterpret_cast<const uint4*>(pv + (uint32_t)((v_first + 64 * i + lane) * 16));
     };
 
     // ---- queries of the wave's rows ----
@@ -327,11 +331,11 @@ __global__ __launch_bounds__(kWaves * 64, 2) void tree_tiles_kernel(const TreeMf
     int row_node[kTiles];
 #pragma unroll
     for (int nr = 0; nr < kTiles; ++nr) {
-      const int row = rt * kRows + (rg * kTiles + nr) * 16 + n16, node = row / G, head = row - node * G;
+      const int row = rt * kRows + (rg * kTiles + nr) * 16 + n16, node = row / a.G, head = row - node * a.G;
       const bool there = node < min(r.T, ta.max_q);
       row_node[nr] = there ? min(node, MEPIC_TREE_MAX_NODES - 1) : 0;
       float x[kSteps][8];
-      const uint16_t* src = static_cast<const uint16_t*>(a.q) + ((size_t)(r.q0 + row_node[nr]) * a.Hq + (size_t)hk * G + head) * D;
+      const uint16_t* src = static_cast<const uint16_t*>(a.q) + ((size_t)(r.q0 + row_node[nr]) * a.Hq + (size_t)hk * a.G + head) * D;
       const float pos = there ? (float)(int)((uint32_t)a.q_positions[r.q0 + row_node[nr]] - (uint32_t)base) : 0.f;
 #pragma unroll
       for (int kk = 0; kk < kSteps; ++kk) {
@@ -758,66 +762,99 @@ __global__ __launch_bounds__(kWaves * 64, 2) void tree_tiles_kernel(const TreeMf
       }
     }
 
-    // ---- the waves of a group of rows merged, rows written ----
+    // ---- rows written; where several waves share a row's slots, they are merged first ----
     const int rows_here = min(n_rows, kRows);
-    if (busy) {
-#pragma unroll
-      for (int nr = 0; nr < kTiles; ++nr) {
-        const float total_w = kFp8 ? sum_over_kgroups(sum[nr]) : ones[nr][0];
-        const float low = -max_over_kgroups(-least[nr]);
-        const int row = nr * 16 + n16;
-        if (g == 0) {
-          tail.ml[wave][row][0] = top[nr];
-          tail.ml[wave][row][1] = low == -INFINITY ? NAN : total_w;
-        }
-        float* dst = reinterpret_cast<float*>(lds) + (size_t)(wave * kTiles * 16 + row) * D;
-#pragma unroll
-        for (int dt = 0; dt < kDims; ++dt) *reinterpret_cast<floatx4*>(dst + 4 * ((4 * dt + g) ^ n16)) = o[nr][dt];
-      }
-    }
-    for (int i = tid; i < kRows; i += kThreads) tail.bad[i] = 0;
-    __syncthreads();
     const bool direct = t0 == 0 && t1 == tiles;
-    constexpr int kQuads = D / 4;
     const size_t part = ((size_t)blockIdx.x * 2 + (t0 == 0 ? 1 : 0)) * kRows;
-    for (int u = tid; u < rows_here * kQuads; u += kThreads) {
-      const int row = u / kQuads, quad = u % kQuads, in = row % (16 * kTiles), w0 = row / (16 * kTiles);
-      float mx = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < kSlotGroups; ++i) mx = fmaxf(mx, tail.ml[w0 + i * kGroups][in][0]);
-      float den = 0.f;
-      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-      for (int i = 0; i < kSlotGroups; ++i) {
-        const int w = w0 + i * kGroups;
-        const float mi = tail.ml[w][in][0], li = tail.ml[w][in][1];
-        if (mi == -INFINITY && li == 0.f) continue;  // no slot took part
-        const float f = mi == mx ? 1.f : __builtin_amdgcn_exp2f(mi - mx);
-        const float4 y = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(lds) + (size_t)(w * kTiles * 16 + in) * D + 4 * (quad ^ (in & 15)));
-        den += f * li;
-        x.x += f * y.x; x.y += f * y.y; x.z += f * y.z; x.w += f * y.w;
-      }
+    // four dims of a row: its output, divided by the sum of weights, or its partial
+    auto put = [&](int row, int dim, const floatx4& x, float mx, float den, float inv, uint16_t* out) {
       if (direct) {
-        const int all = rt * kRows + row, node = all / G, head = all - node * G;
-        const float inv = den != 0.f ? 1.f / den : 0.f;
         uint2 w;
-        w.x = pack2_bf16(x.x * inv, x.y * inv);
-        w.y = pack2_bf16(x.z * inv, x.w * inv);
-        __builtin_memcpy(static_cast<uint16_t*>(a.out) + ((size_t)(r.q0 + node) * a.Hq + (size_t)hk * G + head) * D + 4 * quad, &w, 8);
-        const float odd = (x.x + x.y + x.z + x.w) * 0.f + den * 0.f;  // NaN if anything is Inf or NaN
-        if (!(odd == 0.f)) tail.bad[row] = 1;
+        w.x = pack2_bf16(x[0] * inv, x[1] * inv);
+        w.y = pack2_bf16(x[2] * inv, x[3] * inv);
+        __builtin_memcpy(out + dim, &w, 8);
       } else {
-        *reinterpret_cast<float4*>(m.part_o + (part + row) * D + 4 * quad) = x;
-        if (quad == 0) *reinterpret_cast<float2*>(m.part_ml + (part + row) * 2) = make_float2(mx, den);
+        *reinterpret_cast<floatx4*>(tail.part_o + (part + row) * D + dim) = x;
+        if (dim == 0) *reinterpret_cast<float2*>(tail.part_ml + (part + row) * 2) = make_float2(mx, den);
+      }
+    };
+    auto out_of = [&](int row) {
+      const int all = rt * kRows + row, node = all / a.G, head = all - node * a.G;
+      return static_cast<uint16_t*>(a.out) + ((size_t)(r.q0 + node) * a.Hq + (size_t)hk * a.G + head) * D;
+    };
+    auto mark = [&](int row, float odd) {  // odd is NaN if anything is Inf or NaN
+      if (direct && !(odd == 0.f)) atomicOr(&tail.bad[row >> 5], 1u << (row & 31));
+    };
+    if constexpr (kSlotGroups == 1) {
+      if (busy) {
+#pragma unroll
+        for (int nr = 0; nr < kTiles; ++nr) {
+          const int row = (wave * kTiles + nr) * 16 + n16;
+          const float total_w = kFp8 ? sum_over_kgroups(sum[nr]) : ones[nr][0];
+          const float den = -max_over_kgroups(-least[nr]) == -INFINITY ? NAN : total_w;
+          if (row < rows_here) {
+            const bool none = top[nr] == -INFINITY && den == 0.f;  // no slot took part
+            const float inv = den != 0.f ? 1.f / den : 0.f;
+            uint16_t* out = out_of(row);
+            float odd = den * 0.f;
+#pragma unroll
+            for (int dt = 0; dt < kDims; ++dt) {
+              const floatx4 x = none ? floatx4{0.f, 0.f, 0.f, 0.f} : o[nr][dt];
+              odd += (x[0] + x[1] + x[2] + x[3]) * 0.f;
+              put(row, 16 * dt + 4 * g, x, top[nr], den, inv, out);
+            }
+            mark(row, odd);
+          }
+        }
+      }
+    } else {
+      if (busy) {
+#pragma unroll
+        for (int nr = 0; nr < kTiles; ++nr) {
+          const float total_w = kFp8 ? sum_over_kgroups(sum[nr]) : ones[nr][0];
+          const float low = -max_over_kgroups(-least[nr]);
+          const int row = nr * 16 + n16;
+          if (g == 0) {
+            tail.ml[wave][row][0] = top[nr];
+            tail.ml[wave][row][1] = low == -INFINITY ? NAN : total_w;
+          }
+          float* dst = reinterpret_cast<float*>(lds) + (size_t)(wave * kTiles * 16 + row) * D;
+#pragma unroll
+          for (int dt = 0; dt < kDims; ++dt) *reinterpret_cast<floatx4*>(dst + 4 * ((4 * dt + g) ^ n16)) = o[nr][dt];
+        }
+      }
+      __syncthreads();
+      constexpr int kQuads = D / 4;
+      for (int u = tid; u < rows_here * kQuads; u += kThreads) {
+        const int row = u / kQuads, quad = u % kQuads, in = row % (16 * kTiles), w0 = row / (16 * kTiles);
+        float mx = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < kSlotGroups; ++i) mx = fmaxf(mx, tail.ml[w0 + i * kGroups][in][0]);
+        float den = 0.f;
+        floatx4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < kSlotGroups; ++i) {
+          const int w = w0 + i * kGroups;
+          const float mi = tail.ml[w][in][0], li = tail.ml[w][in][1];
+          if (mi == -INFINITY && li == 0.f) continue;  // no slot took part
+          const float f = mi == mx ? 1.f : __builtin_amdgcn_exp2f(mi - mx);
+          const floatx4 y = *reinterpret_cast<const floatx4*>(reinterpret_cast<const float*>(lds) + (size_t)(w * kTiles * 16 + in) * D + 4 * (quad ^ (in & 15)));
+          den += f * li;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) x[j] += f * y[j];
+        }
+        put(row, 4 * quad, x, mx, den, den != 0.f ? 1.f / den : 0.f, out_of(row));
+        mark(row, (x[0] + x[1] + x[2] + x[3]) * 0.f + den * 0.f);
       }
     }
     __syncthreads();
-    if (direct) {
-      for (int row = 0; row < rows_here; ++row) {
-        if (!tail.bad[row]) continue;
-        const int all = rt * kRows + row, node = all / G, head = all - node * G;
-        tree_row<kFp8 ? MEPIC_F8E4M3 : MEPIC_BF16, kThreads>(ta, tail.row, r, b, node, hk * G + head);
+    for (int w = 0; direct && w < kRows / 32; ++w) {
+      const uint32_t all_bits = uni(tail.bad[w]);
+      for (uint32_t bits = all_bits; bits; bits &= bits - 1) {
+        const int all = rt * kRows + 32 * w + __builtin_ctz(bits), node = all / a.G, head = all - node * a.G;
+        tree_row<kFp8 ? MEPIC_F8E4M3 : MEPIC_BF16, kThreads>(ta, tail.row, r, b, node, hk * a.G + head);
       }
+      if (all_bits && tid == 0) tail.bad[w] = 0;  // (tree_row has barriers: every wave has read it)
     }
     at += m.whole ? 1 : t1 - t0;
   }
