@@ -313,7 +313,8 @@ int run_tree(const mepic_attn_params* p, const int32_t* parents, void* hip_strea
   t.max_q = max_q;
   int max_kv = p->max_kv_len > 0 ? p->max_kv_len : p->max_blocks * p->P;
   if (max_kv > p->max_blocks * p->P) max_kv = p->max_blocks * p->P;
-  const TreePlan pl = p->kv_dtype == MEPIC_F32 || (p->flags & MEPIC_FLAG_FORCE_GENERAL) ? TreePlan{} : tree_mfma_plan(t, max_kv);
+  const bool f32 = p->kv_dtype == MEPIC_F32;
+  const TreePlan pl = p->flags & MEPIC_FLAG_FORCE_GENERAL ? TreePlan{} : f32 ? tree_f32_plan(t, max_kv) : tree_mfma_plan(t, max_kv);
   const size_t need = pl.bytes;
   if (bytes_only) {
     *bytes_only = need;
@@ -343,7 +344,11 @@ int run_tree(const mepic_attn_params* p, const int32_t* parents, void* hip_strea
   hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
   hipError_t e;
   mark(a.timing_start, s);
-  if (pl.rows) {
+  if (pl.rows && f32) {
+    g_last_kernel = "tree_mfma_f32";
+    e = launch_tree_f32(t, pl, p->workspace, s);
+    mark(a.timing_stop, s);
+  } else if (pl.rows) {
     g_last_kernel = p->kv_dtype == MEPIC_F8E4M3 ? "tree_mfma_fp8" : "tree_mfma_bf16";
     e = launch_tree_mfma(t, pl, p->workspace, s);
   } else {

@@ -37,6 +37,19 @@ __device__ __forceinline__ int tree_parent(const int32_t* parents, int q0, int j
   return p >= 0 && p < j ? p : -1;
 }
 
+// The low n bits, n from anything below 0 to anything above 32.
+__device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u; }
+
+// Bits of slots n0 .. n0 + 31 that a row sees: all of the context's, of the nodes those on its path.
+__device__ __forceinline__ uint32_t path_bits(const uint32_t* path, int n0, int ctx) {
+  const int off = n0 - ctx;  // bit i is node off + i
+  if (off <= -32) return ~0u;
+  if (off < 0) return low_bits(-off) | (path[0] << -off);
+  const int w = off >> 5, s = off & 31;
+  const uint32_t lo = w < kTreeWords ? path[w] >> s : 0u;
+  return s && w + 1 < kTreeWords ? lo | (path[w + 1] << (32 - s)) : lo;
+}
+
 template <int kThreads>
 struct TreeRowLds {
   float qhat[2 * kMaxHalfD];  // rotated, times scale log2(e)
@@ -191,6 +204,7 @@ struct TreePlan {
   int groups;      // workgroups per KV head
   int min_slots;   // least run of a workgroup
   bool whole;      // a workgroup takes whole items (row tiles of a request): nothing to merge
+  int row_tiles, splits;  // fp32 pages: row tiles per request, workgroups per item
   size_t bytes;    // workspace
 };
 
@@ -202,6 +216,15 @@ struct TreeMfmaArgs {
   int4* row_wgs;     // [n_q * G] first and last workgroup (of a KV head) that a row's item is cut for, row of the tile, request
 };
 
+struct TreeF32Args {
+  TreeArgs t;
+  int32_t row_tiles, splits;
+  float* part_o;   // [B * row_tiles][splits][Hkv][16][D]
+  float* part_ml;  // [B * row_tiles][splits][Hkv][16][2]
+};
+
+TreePlan tree_f32_plan(const TreeArgs& t, int max_kv);
+hipError_t launch_tree_f32(const TreeArgs& t, const TreePlan& pl, void* workspace, hipStream_t s);
 TreePlan tree_mfma_plan(const TreeArgs& t, int max_kv);  // reads shapes and max_q; rows = 0: the general kernel's
 hipError_t launch_tree_mfma(const TreeArgs& t, const TreePlan& pl, void* workspace, hipStream_t s);  // bf16 or e4m3 pages; with its merge and timing_stop
 hipError_t launch_tree_tiles_bf16(int rows, const TreeMfmaArgs& m, hipStream_t s);

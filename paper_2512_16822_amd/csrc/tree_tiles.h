@@ -59,19 +59,6 @@ __device__ __forceinline__ uint32_t f16_of_e4m3(uint32_t w, bool high) {
   return __builtin_bit_cast(uint32_t, high ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, true) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, false));
 }
 
-// The low n bits, n from anything below 0 to anything above 32.
-__device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u; }
-
-// Bits of slots n0 .. n0 + 31 that a row sees: all of the context's, of the nodes those on its path.
-__device__ __forceinline__ uint32_t path_bits(const uint32_t* path, int n0, int ctx) {
-  const int off = n0 - ctx;  // bit i is node off + i
-  if (off <= -32) return ~0u;
-  if (off < 0) return low_bits(-off) | (path[0] << -off);
-  const int w = off >> 5, s = off & 31;
-  const uint32_t lo = w < kTreeWords ? path[w] >> s : 0u;
-  return s && w + 1 < kTreeWords ? lo | (path[w + 1] << (32 - s)) : lo;
-}
-
 template <bool kFp8, int D, int kWaves, int kGroups, int kTiles, bool kPlain>
 __global__ __launch_bounds__(kWaves * 64, 2) void tree_tiles_kernel(const TreeMfmaArgs m) {
   constexpr int kThreads = kWaves * 64, kTile = 16 * kWaves;  // slots of a tile
