@@ -21,7 +21,8 @@ hipError_t launch_rows(int rows, const TreeMfmaArgs& m, hipStream_t s) {
   if (rows == 32) return launch_one<D, 8, 2, 1, kPlain>(m, s);
   if (rows == 64) return launch_one<D, 4, 4, 1, kPlain>(m, s);
   if (rows == 128) return launch_one<D, 4, 4, 2, kPlain>(m, s);
-  return launch_one<D, 8, 8, 2, kPlain>(m, s);
+  if (rows == 256) return launch_one<D, 8, 8, 2, kPlain>(m, s);
+  return hipErrorInvalidValue;  // (a plan for other rows has a workspace of other sizes)
 }
 
 }  // namespace
