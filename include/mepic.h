@@ -431,8 +431,10 @@ int mepic_attn_decode_batched(const mepic_attn_params* params, const int32_t* pl
  * params as for mepic_attn_prefill (cu_q_lens and max_q_len as there; MEPIC_FLAG_FORCE_GENERAL runs plain fp32 arithmetic).
  * Rows behind cu_q_lens[B] are left as they were. A row that sees no slot is all zeros. A request of more than max_q_len nodes, or
  * of fewer slots than nodes, gives unspecified rows, never a fault. What a row does not see may hold anything, NaN and Inf included.
- * 16-bit pages: keys are rotated in fp32 and enter matrix products as fp16 (11 significant bits), bf16 probabilities meet bf16 V as stored;
- * e4m3 pages: everything in fp16. A row that comes out Inf or NaN is computed again in plain fp32 arithmetic.
+ * fp32 pages: fp32 operands throughout. bf16 pages: rotated keys and queries enter matrix products as fp16 (11 significant bits; keys may also be
+ * rotated in fp16, each product and sum rounded), bf16 probabilities meet bf16 V as stored; e4m3 pages: everything in fp16, codes
+ * exactly. Sums are fp32. A row that comes out Inf or NaN is computed again in plain fp32 arithmetic. MEPIC_FLAG_KV_READ_ONCE is accepted and changes nothing.
+ * Results do not depend on what else runs: no atomics, one order of sums for given lengths, trees and shapes of the call.
  * Errors: as mepic_attn_prefill, and MEPIC_ERR_UNSUPPORTED for max_q_len > MEPIC_TREE_MAX_NODES.
  */
 int mepic_attn_tree(const mepic_attn_params* params, const int32_t* parents, void* hip_stream);

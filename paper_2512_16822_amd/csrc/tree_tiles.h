@@ -2,20 +2,27 @@
 // files instantiate.
 //
 // A verification step brings R = nodes x (Hq / Hkv) query rows per KV head to the same context: 8 to 512 where decode has 1 to 16. So
-// a key is rotated once per tile of rows and shared through LDS, and HBM bounds the call up to some 128 rows.
-//   * Work. An item is a tile of kRows rows of one request; its keys come in tiles of 128 slots. The (item, tile) pairs of a KV head form
-//     one sequence that the head's workgroups (one per compute unit, 8 waves) cut into equal runs; a row cut in two
-//     or more goes through partials and tree_merge_kernel, any other is written directly.
-//   * Staging. A wave has eight rotary pairs, a lane one or two slots. cos and sin of its slot's position stay in registers and are
-//     turned on from slot to slot, 64 or 128 positions on (the turn is the same for a wave: scalar registers), found anew every 16 tiles and
-//     where positions jump. K goes to LDS as fp16 in operand order, V as matrix operands too (e4m3 widened to fp16, which holds the codes
-//     exactly); the loads of the next tile are in flight during the products of this one.
+// a key is rotated once per tile of rows and shared through LDS. What bounds it is vector work: of 64 requests x 4.3 K slots x 64 rows (163 us, 443
+// TFLOP/s) the vector units are busy 55 % of the time, with two waves a SIMD that wait 29 % of theirs, mostly at a tile's barrier, LDS 37 %,
+// the matrix cores 22 %. With 24 rows, 8 x 65 K slots, it is memory: 376 us, 5.7 TB/s.
+//   * Work. An item is a tile of kRows rows of one request; its keys come in tiles of kTile = 16 kWaves slots. The (item, tile) pairs of a KV head
+//     form one sequence that the head's workgroups cut into equal runs; a row cut in two or more goes through partials and
+//     tree_merge_kernel, any other is written directly. With four waves two workgroups share a compute unit and fill each other's waits (64 rows,
+//     when it was chosen: 178 us; one of eight waves and twice the tile 191).
+//   * Staging. A wave has an octet of rotary pairs (or two), a lane one slot or two. K goes to LDS as fp16 in operand order, V as matrix operands too (e4m3
+//     widened to fp16, which holds the codes exactly); the loads of the next tile are in flight during the products of this one, ids,
+//     masks and scales ahead of keys and values.
+//   * Rotation, in general: cos and sin of its slot's position stay in a lane's registers in fp32 and are turned on from slot to slot (the turn is
+//     the same for a wave: scalar registers), found anew every 16 tiles and where positions jump. Tiles of 64 rows without masks, positions
+//     or interleaving (kWindows): a window of two tiles starts at position 0 for its keys, whose cos and sin are then the same in every window and kept as packed fp16,
+//     and the queries, kept in fp32, are turned back by a window's length instead: 171 us against 182 when both were
+//     measured, at 2 us more before a workgroup's first tile. With 32 rows there is too little else to do for that to pay: 8 x 65 K slots 376 us without, 407 with.
 //   * Products. S^T[32 slots x 16 rows] = K Q^T with v_mfma_f32_16x16x32_f16 and O^T[dims x rows] += V^T P^T: a lane owns one row, so
 //     sums, maxima and rescaling are its own. Slots are laid out so that the scores a lane gets are the eight consecutive slots its
-//     operand of P^T needs. kGroups groups of waves take 16 kTiles rows each; waves of a group share the tile's slots and are merged in
-//     LDS at the end of a run.
-//   * Precision. Query rows are scaled by a power of two to at most 1 and keys times 16 (e4m3 codes as they are), both in fp16: 11
-//     significant bits where bf16 has 8; a key beyond 2896 gives an infinite score, which marks the row. P is bf16 next to bf16 V, fp16
+//     operand of P^T needs. kGroups groups of waves take 16 kTiles rows each; where several waves share a group's rows, they have different slots
+//     and are merged in LDS at the end of a run.
+//   * Precision. Query rows are scaled by a power of two to at most 1 and keys times 16 (kWindows and e4m3 codes: as they are), both in fp16: 11
+//     significant bits where bf16 has 8; a key beyond 2896 (46340) gives an infinite score, which marks the row. P is bf16 next to bf16 V, fp16
 //     next to e4m3 V, where the exponent of the page's V scale joins the score and its mantissa P. Sums and O are fp32. The reference maximum
 //     of a row lags by up to 8 (log2 units).
 //   * A marked row, or one that came out Inf or NaN, is computed again by tree_row.
