@@ -6,7 +6,7 @@
 // TFLOP/s) the vector units are busy 55 % of the time, with two waves a SIMD that wait 29 % of theirs, mostly at a tile's barrier, LDS 37 %,
 // the matrix cores 22 %. With 24 rows, 8 x 65 K slots, it is memory: 376 us, 5.7 TB/s.
 //   * Work. An item is a tile of kRows rows of one request; its keys come in tiles of kTile = 16 kWaves slots. The (item, tile) pairs of a KV head
-//     form one sequence that the head's workgroups cut into equal runs; a row cut in two or more goes through partials and
+//     form one sequence that the head's workgroups cut into equal runs (an item's start counts for some tiles too); a row cut in two or more goes through partials and
 //     tree_merge_kernel, any other is written directly. With four waves two workgroups share a compute unit and fill each other's waits (64 rows,
 //     when it was chosen: 178 us; one of eight waves and twice the tile 191).
 //   * Staging. A wave has an octet of rotary pairs (or two), a lane one slot or two. K goes to LDS as fp16 in operand order, V as matrix operands too (e4m3
@@ -81,6 +81,10 @@ __global__ __launch_bounds__(kWaves * 64, 2) void tree_tiles_kernel(const TreeMf
   constexpr int kVGranules = 16 * D * E / 16 / 64;        // 16-byte pieces of V per lane and tile
   constexpr int kRing = kTiles == 1 && D == 128 ? 8 : 4;  // operands in flight: some 150 clocks a read, 16 a product
   constexpr bool kWindows = kPlain && kTiles == 1 && kSlotGroups == 1;  // keys turned from the start of a window of two tiles (see Staging)
+  // What the start of an item (queries, paths, first loads) counts for in tiles, where workgroups are given equal parts: 256 slots' worth, which a tile of
+  // 256 rows takes as long for as for a start. Without it whoever has the joint of two requests ends last: 4 x 1.7 K slots 26.2 us and 20.9, 16 x 0.5 - 3.1 K in
+  // a whole step 73.0 and 68.5, 128 x 2 - 33 K e4m3 825 and 810; 256 rows 332 without, 336 with.
+  constexpr int kStart = kRows == 256 ? 0 : 256 / kTile;
   constexpr float kKeyFactor = kFp8 || kWindows ? 1.f : 16.f;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   TreeLdsTail<kWaves>& tail = *reinterpret_cast<TreeLdsTail<kWaves>*>(lds + 2 * kTileBytes);
@@ -114,7 +118,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void tree_tiles_kernel(const TreeMf
     const TreeRequest r = tree_request(a, b);
     tiles = max((r.kv_len + kTile - 1) / kTile, 1);
     items = (min(r.T, ta.max_q) * G + kRows - 1) / kRows;
-    return m.whole ? items : items * tiles;
+    return m.whole ? items : items * (tiles + kStart);
   };
   // inclusive prefix sums of the costs of kThreads requests; returns their total
   auto scan_costs = [&](int b0, int& incl, int& cost) {
@@ -244,15 +248,17 @@ __global__ __launch_bounds__(kWaves * 64, 2) void tree_tiles_kernel(const TreeMf
       if (++b >= a.B) return;
       continue;
     }
-    const int rt = m.whole ? at - before : (at - before) / tiles;
-    const int t0 = m.whole ? 0 : at - before - rt * tiles;
-    const int t1 = m.whole ? tiles : min(tiles, t0 + end - at);
+    const int units = m.whole ? 1 : tiles + kStart, rt = (at - before) / units, unit = at - before - rt * units;
+    const int stop = min(units, unit + end - at);  // the run's units of the item are unit .. stop - 1
+    const int t0 = m.whole ? 0 : max(unit - kStart, 0), t1 = m.whole ? tiles : stop - kStart;
+    at += stop - unit;
+    if (t1 <= t0) continue;  // none of its tiles
     const int n_rows = min(r.T, ta.max_q) * G - rt * kRows;  // rows from the item's first to the request's last
     const size_t bt_row = (size_t)b * a.max_blocks;
 
     // rows that other workgroups share: which ones (head 0 says so for all)
     if (!m.whole && t0 == 0 && hk == 0) {
-      const int last = (before + rt * tiles + tiles - 1) / per;
+      const int last = (before + (rt + 1) * units - 1) / per;
       for (int i = tid; i < min(n_rows, kRows); i += kThreads) {
         m.row_wgs[(size_t)r.q0 * G + rt * kRows + i] = make_int4(wg, last, i, b);
       }
@@ -850,7 +856,6 @@ __global__ __launch_bounds__(kWaves * 64, 2) void tree_tiles_kernel(const TreeMf
       }
       if (all_bits && tid == 0) tail.bad[w] = 0;  // (tree_row has barriers: every wave has read it)
     }
-    at += m.whole ? 1 : t1 - t0;
   }
 }
 
