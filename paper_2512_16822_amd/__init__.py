@@ -447,8 +447,11 @@ def attn_tree_workspace_size(params: AttnParams) -> int:
 def attn_tree(params: AttnParams, parents=None, stream=None) -> None:
     """mepic_attn_tree on `stream` (default: torch's current stream). params: make_params with cu_q_lens and max_q_len; parents:
     int32 tensor [n_q_tokens] on the GPU, None for chains."""
-    if parents is not None and (parents.numel() != params.n_q_tokens or parents.element_size() != 4):
-        raise ValueError(f"parents: int32 of shape ({params.n_q_tokens},) expected, got {parents.dtype} of shape {tuple(parents.shape)}")
+    if parents is not None:
+        import torch
+        if parents.dtype != torch.int32 or parents.dim() != 1 or len(parents) != params.n_q_tokens or not parents.is_cuda or not parents.is_contiguous():
+            raise ValueError(f"parents: contiguous int32 of shape ({params.n_q_tokens},) on the GPU expected, got {parents.dtype} of shape "
+                             f"{tuple(parents.shape)} on {parents.device}")
     rc = load().mepic_attn_tree(ctypes.byref(params), _p(parents), _stream_handle(stream))
     if rc != OK:
         raise MepicError(rc, "mepic_attn_tree")

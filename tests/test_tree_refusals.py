@@ -41,3 +41,10 @@ def test_workspace_size_and_the_binding(mepic):
         mepic.attn_tree(params(mepic), torch.zeros(19, dtype=torch.int32))
     with pytest.raises(ValueError):
         mepic.attn_tree(params(mepic), torch.zeros(20, dtype=torch.int64))
+
+
+def test_parents_elsewhere_or_of_another_kind(mepic):
+    """The kernel would read whatever lies at a host address, or every other number: refused before the call."""
+    for parents in (torch.zeros(20, dtype=torch.int32), torch.zeros(20), torch.zeros(4, 5, dtype=torch.int32), torch.zeros(40, dtype=torch.int32)[::2]):
+        with pytest.raises(ValueError):
+            mepic.attn_tree(params(mepic), parents)
