@@ -435,7 +435,8 @@ int mepic_attn_decode_batched(const mepic_attn_params* params, const int32_t* pl
  * rotated in fp16, each product and sum rounded), bf16 probabilities meet bf16 V as stored; e4m3 pages: everything in fp16, codes
  * exactly. Sums are fp32. A row that comes out Inf or NaN is computed again in plain fp32 arithmetic. MEPIC_FLAG_KV_READ_ONCE is accepted and changes nothing.
  * Results do not depend on what else runs: no atomics, one order of sums for given lengths, trees and shapes of the call.
- * Errors: as mepic_attn_prefill, and MEPIC_ERR_UNSUPPORTED for max_q_len > MEPIC_TREE_MAX_NODES.
+ * Errors: as mepic_attn_prefill, and MEPIC_ERR_UNSUPPORTED for max_q_len > MEPIC_TREE_MAX_NODES and for n_q_tokens * Hq or max_blocks * P beyond
+ * 2^31 - 1.
  */
 int mepic_attn_tree(const mepic_attn_params* params, const int32_t* parents, void* hip_stream);
 

@@ -305,7 +305,7 @@ int run_tree(const mepic_attn_params* p, const int32_t* parents, void* hip_strea
   const int rc = check_shapes(p, true);
   if (rc != MEPIC_OK) return rc;
   const int max_q = p->max_q_len > 0 && p->max_q_len < p->n_q_tokens ? p->max_q_len : p->n_q_tokens;
-  if (max_q > MEPIC_TREE_MAX_NODES || (long)p->n_q_tokens * p->Hq > INT_MAX) return MEPIC_ERR_UNSUPPORTED;
+  if (max_q > MEPIC_TREE_MAX_NODES || (long)p->n_q_tokens * p->Hq > INT_MAX || (long)p->max_blocks * p->P > INT_MAX) return MEPIC_ERR_UNSUPPORTED;
   TreeArgs t{};
   AttnArgs& a = t.a;
   a.B = p->B; a.n_q = p->n_q_tokens; a.Hq = p->Hq; a.Hkv = p->Hkv; a.D = p->D; a.P = p->P;

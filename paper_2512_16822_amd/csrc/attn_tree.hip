@@ -131,7 +131,9 @@ TreePlan tree_mfma_plan(const TreeArgs& t, int max_kv) {
   const int resident = p.rows == 32 || p.rows == 256 ? cus : 2 * cus;  // workgroups of eight and of four waves
   p.groups = resident / a.Hkv > 1 ? resident / a.Hkv : 1;
   const long tiles = (max_kv + 63) / 64;
-  if (((long)a.n_q * a.G / p.rows + a.B + 1) * (tiles + 8) > (1L << 30)) return TreePlan{};  // (the work is counted in 32 bits)
+  // (the work is counted in 32 bits, whatever lengths the device brings: the table's width bounds them, max_kv_len is the caller's word)
+  const long widest = ((long)a.max_blocks * a.P + 63) / 64;
+  if (((long)a.n_q * a.G / p.rows + a.B + 1) * (widest + 8) > (1L << 30)) return TreePlan{};
   // Short contexts are not cut, there is nothing to merge then: us uncut and cut, 4 requests of 80 slots 12.5 and 23.0, of 470 17.5 and 18.7, of 920 24.5 and
   // 20.0; 32 of 470 21.7 and 27.1. A run has 256 slots or more: runs of 128, 256 and 512 take 17.0, 18.6, 20.6 us for one request of 1.2 K, 22.2,
   // 21.6, 28.4 for four of 1.7 K, 33.9, 33.2, 33.6 for four of 4.3 K.

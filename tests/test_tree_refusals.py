@@ -43,6 +43,14 @@ def test_workspace_size_and_the_binding(mepic):
         mepic.attn_tree(params(mepic), torch.zeros(20, dtype=torch.int64))
 
 
+def test_tables_wider_than_slots_can_be_numbered(mepic):
+    call = lambda **o: mepic.load().mepic_attn_tree(ctypes.byref(params(mepic, **o)), None, None)  # noqa: E731
+    assert call(max_blocks=1 << 27) == call(max_blocks=1 << 27, max_kv_len=100) == call(n_q_tokens=1 << 28, max_q_len=8) == mepic.ERR_UNSUPPORTED
+    # the largest table that can be: the work of the matrix-core kernels still fits 32 bits for two requests, not for a thousand
+    assert mepic.attn_tree_workspace_size(params(mepic, max_blocks=(1 << 27) - 1, max_kv_len=5000)) > 0
+    assert mepic.attn_tree_workspace_size(params(mepic, max_blocks=(1 << 27) - 1, max_kv_len=5000, B=1000, n_q_tokens=8000)) == 0
+
+
 def test_parents_elsewhere_or_of_another_kind(mepic):
     """The kernel would read whatever lies at a host address, or every other number: refused before the call."""
     for parents in (torch.zeros(20, dtype=torch.int32), torch.zeros(20), torch.zeros(4, 5, dtype=torch.int32), torch.zeros(40, dtype=torch.int32)[::2]):
