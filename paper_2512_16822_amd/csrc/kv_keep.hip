@@ -4,7 +4,9 @@
 //
 // One workgroup per (request, KV head) takes groups of kGroup tokens: slots and pages of the group are resolved into LDS, all its
 // granules of K and elements of V are requested, and after a barrier stored. Bound by the chain of dependent loads (prefix sums,
-// node, block table, scale, K/V): the bytes are few.
+// node, block table, scale, K/V), each some 2 us with what starts and ends a launch: the bytes are few. Measured: 64 requests with 26 drafted tokens
+// at most 16.3 - 17.5 us, 1024 with 64 on e4m3 pages 21.2. Lanes across the dims of one token leave whole waves out of tokens that are not
+// there; across the tokens of one dim, whose elements of V are neighbours, the same calls take 17.6 and 26.3.
 #include "attn_common.h"
 
 namespace mepic {
